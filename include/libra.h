@@ -445,6 +445,93 @@ int libra_kv_scatter(libra_handle_t handle, const void* k_dense, const void* v_d
                      int32_t head_begin, int32_t head_count, void* k_pages, void* v_pages, void* error_word_dev,
                      void* stream);
 
+/* ---- Chunks of new tokens: rotary positions, append to the pages, attention over them --------------------------------
+ * A trajectory grows by more than a token at a time when it starts (its prompt) and at every tool return (Section 2.2
+ * of the paper).  The calls below absorb such chunks: libra_rope_append rotates the new tokens' q and k and writes k and v
+ * into the pages.  The new tokens of a batch are packed: those of sequence b are rows
+ * q_offsets[b] .. q_offsets[b + 1] - 1 of q, in order, and seq_lens[b] counts them, so that row q_offsets[b] + i is token
+ * seq_lens[b] - q_len_b + i of its sequence (q_len_b = q_offsets[b + 1] - q_offsets[b]; 0 is allowed). */
+
+/* Rotary positions.  Pair i (0 <= i < rotary_dim / 2) of a head's channels is rotated by pos * theta_i:
+ *     (x, y) -> magnitude * (x cos a - y sin a, x sin a + y cos a),   a = pos * theta_i,   theta_i = base^(-2 i / rotary_dim)
+ * LIBRA_ROPE_HALF: the pair is channels i and i + rotary_dim / 2; LIBRA_ROPE_INTERLEAVED: channels 2 i and 2 i + 1.
+ * Channels from rotary_dim on pass through unchanged.  For contexts longer than a model was trained on the angles are scaled
+ * (factor >= 1):
+ *   LINEAR  theta_i / factor
+ *   BASE    base * factor^(R / (R - 2)) takes base's place (R = rotary_dim > 2)
+ *   BANDS   with n_i = original_len * theta_i / (2 pi), the turns made within original_len tokens:
+ *           keep = clamp((n_i - low) / (high - low), 0, 1);   theta_i * keep + theta_i / factor * (1 - keep)
+ *   RAMP    pair(n) = R ln(original_len / (2 pi n)) / (2 ln base);  lo = max(floor(pair(high)), 0),
+ *           hi = min(ceil(pair(low)), R - 1);  gone = clamp((i - lo) / max(hi - lo, 0.001), 0, 1);
+ *           theta_i * (1 - gone) + theta_i / factor * gone
+ * magnitude 0 = the default: 0.1 ln(factor) + 1 for RAMP, else 1.  low, high, original_len are read by BANDS and RAMP only.
+ *
+ * libra_rope_t is plain host data (copy it freely); libra_rope_init fills it and needs no GPU.  The angles are held in
+ * turns as 0.64 fixed-point numbers: pos * theta is then exact modulo one turn for every 32-bit position, negative
+ * ones too.  scaling NULL = none.  Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (rotary_dim > 256). */
+#define LIBRA_ROPE_HALF 0
+#define LIBRA_ROPE_INTERLEAVED 1
+#define LIBRA_ROPE_SCALE_NONE 0
+#define LIBRA_ROPE_SCALE_LINEAR 1
+#define LIBRA_ROPE_SCALE_BASE 2
+#define LIBRA_ROPE_SCALE_BANDS 3
+#define LIBRA_ROPE_SCALE_RAMP 4
+#define LIBRA_ROPE_MAX_PAIRS 128
+typedef struct {
+  int32_t kind;          /* LIBRA_ROPE_SCALE_*                                                    */
+  int32_t original_len;  /* tokens                                                                */
+  double factor;
+  double low, high;      /* turns                                                                 */
+  double magnitude;
+} libra_rope_scaling_t;
+typedef struct {
+  int32_t rotary_dim;
+  int32_t layout;        /* LIBRA_ROPE_HALF / LIBRA_ROPE_INTERLEAVED                              */
+  float magnitude;
+  int32_t reserved;
+  uint64_t turns[LIBRA_ROPE_MAX_PAIRS]; /* turns per position of pair i, in units of 2^-64          */
+} libra_rope_t;
+int libra_rope_init(libra_rope_t* rope, int32_t rotary_dim, int32_t layout, double base,
+                    const libra_rope_scaling_t* scaling);
+
+/* Rotate rows of heads: x and out are device arrays [n_tokens, n_heads, head_dim] of `dtype` on `device`, element
+ * (t, h, c) at t * stride_token + h * stride_head + c; positions is int32[n_tokens] on the device.  direction
+ * LIBRA_ROPE_FORWARD is the map above; LIBRA_ROPE_GRADIENT is its transpose, which takes the gradient of the output to the
+ * gradient of the input (magnitude included).  out may be x (with the same strides); any other overlap is not allowed.
+ * Arithmetic in float32, one rounding to `dtype`.  head_dim is even, rotary_dim <= head_dim <= 1024; rows need no more than the
+ * element's own alignment (16-byte aligned ones are faster).  Asynchronous on `stream`; nothing is allocated.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE, CUDA_ERROR. */
+#define LIBRA_ROPE_BF16 0
+#define LIBRA_ROPE_F16 1
+#define LIBRA_ROPE_F32 2
+#define LIBRA_ROPE_FORWARD 0
+#define LIBRA_ROPE_GRADIENT 1
+int libra_rope_apply(int32_t device, const libra_rope_t* rope, const void* x, void* out, int32_t dtype,
+                     const int32_t* positions, int64_t n_tokens, int32_t n_heads, int32_t head_dim,
+                     int64_t x_stride_token, int64_t x_stride_head, int64_t out_stride_token, int64_t out_stride_head,
+                     int32_t direction, void* stream);
+
+/* Rotate the q and k rows of a packed batch of new tokens and append k and v to the pages, in one pass.
+ *   q, q_out      bf16, row r at r * q_stride (q_out_stride) elements, num_q_heads * head_dim each; q_out may be q (same
+ *                 stride).  Both NULL: only k and v are handled.
+ *   k_new, v_new  bf16, row r at r * kv_stride elements, num_kv_heads * head_dim each
+ *   q_offsets     int32[batch + 1], seq_lens int32[batch], block_table: device pointers, see above
+ *   max_rows      rows the buffers hold; >= q_offsets[batch].  Rows behind q_offsets[batch] are left as they were, so that a
+ *                 recorded call can be replayed with fewer tokens than it was recorded for.
+ * Token t of a sequence goes to slot t % page_size of page block_table[b][t / page_size], rotated by position t; v is
+ * copied.  Over E4M3 pools the rotated k and v are divided by k_scale / v_scale (multiplied by the reciprocal) and
+ * rounded to nearest even from float32, magnitudes beyond the largest code (448) to that code, NaN to the NaN code.
+ * A row at a negative position (a chunk longer than its sequence) gets its q rotated by that position and is not stored.
+ * rope NULL = no rotation (positions applied elsewhere): q is copied if given.  Row buffers 16-byte aligned, strides
+ * multiples of 8; no two rows of a call may name the same slot.  Bits of *error_word_dev (32-bit device word):
+ * LIBRA_ERR_BAD_PAGE_ID for a page id outside the pool, LIBRA_ERR_PLAN_OVERFLOW for a token past the end of a block-table
+ * row; such a token is not stored.  The handle supplies the pool geometry and type; no plan, no workspace.  Asynchronous on
+ * `stream`.  Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (rotary_dim > head_dim), CUDA_ERROR. */
+int libra_rope_append(libra_handle_t handle, const libra_rope_t* rope, const void* q, int64_t q_stride, void* q_out,
+                      int64_t q_out_stride, const void* k_new, const void* v_new, int64_t kv_stride,
+                      const int32_t* q_offsets, const int32_t* seq_lens, const int32_t* block_table, int32_t batch,
+                      int32_t max_rows, void* k_pages, void* v_pages, void* error_word_dev, void* stream);
+
 /* ---- the paper's rollout-side schedulers, host code only (no GPU) ------------------------------------ */
 
 /* RolloutDP of the Global Resource Planner (Section 4.3, Algorithm 1): split `n_gpus` GPUs into inference

@@ -62,6 +62,24 @@ class RingOp(C.Structure):
                 ("piece", C.c_int32), ("peer", C.c_int32), ("offset", C.c_int64), ("bytes", C.c_int64)]
 
 
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_BANDS, ROPE_SCALE_RAMP = range(5)
+ROPE_BF16, ROPE_F16, ROPE_F32 = 0, 1, 2
+ROPE_FORWARD, ROPE_GRADIENT = 0, 1
+ROPE_MAX_PAIRS = 128
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("original_len", C.c_int32), ("factor", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("magnitude", C.c_double)]
+
+
+class Rope(C.Structure):
+    """libra_rope_t: the angles per position of every pair of channels (host data)."""
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float), ("reserved", C.c_int32),
+                ("turns", C.c_uint64 * ROPE_MAX_PAIRS)]
+
+
 _i32p = C.POINTER(C.c_int32)
 _vp = C.c_void_p
 
@@ -118,6 +136,11 @@ SIGNATURES = {
                                   _vp, _vp]),
     "libra_kv_scatter": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp, _vp,
                                    _vp, _vp]),
+    "libra_rope_init": (C.c_int, [C.POINTER(Rope), C.c_int32, C.c_int32, C.c_double, C.POINTER(RopeScaling)]),
+    "libra_rope_apply": (C.c_int, [C.c_int32, C.POINTER(Rope), _vp, _vp, C.c_int32, _vp, C.c_int64, C.c_int32, C.c_int32,
+                                   C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, _vp]),
+    "libra_rope_append": (C.c_int, [_vp, C.POINTER(Rope), _vp, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, _vp,
+                                    C.c_int32, C.c_int32, _vp, _vp, _vp, _vp]),
     "libra_rollout_dp": (C.c_int, [C.c_int32, _i32p, C.c_int32, _i32p, C.c_int32, C.POINTER(C.c_double),
                                    C.POINTER(C.c_double), _i32p, _i32p, _i32p, C.c_int32, _i32p]),
     "libra_trie_create": (C.c_int, [C.POINTER(_vp), _i32p, C.c_int32]),
@@ -239,6 +262,23 @@ def libra_merge_parts(device: int, parts_out_ptr: int, parts_lse_ptr: int, n_par
     """Log-sum-exp merge of (out, lse) pairs computed over disjoint parts of the same sequences."""
     _check(lib.libra_merge_parts(device, parts_out_ptr, parts_lse_ptr, n_parts, rows, head_dim, out_ptr,
                                  lse_out_ptr or None, stream), "libra_merge_parts")
+
+
+def libra_rope_init(rotary_dim: int, layout: int = ROPE_HALF, base: float = 10000.0, scaling: int = ROPE_SCALE_NONE,
+                    factor: float = 1.0, low: float = 0.0, high: float = 0.0, original_len: int = 0,
+                    magnitude: float = 0.0) -> Rope:
+    rope, sc = Rope(), RopeScaling(scaling, original_len, factor, low, high, magnitude)
+    _check(lib.libra_rope_init(C.byref(rope), rotary_dim, layout, base, C.byref(sc)), "libra_rope_init")
+    return rope
+
+
+def libra_rope_apply(device: int, rope: Rope, x_ptr: int, out_ptr: int, dtype: int, positions_ptr: int, n_tokens: int,
+                     n_heads: int, head_dim: int, x_stride_token: int, x_stride_head: int, out_stride_token: int,
+                     out_stride_head: int, direction: int, stream: int) -> None:
+    """Rotary positions (or their gradient) on rows of heads; strides in elements."""
+    _check(lib.libra_rope_apply(device, rope, x_ptr, out_ptr, dtype, positions_ptr, n_tokens, n_heads, head_dim,
+                                x_stride_token, x_stride_head, out_stride_token, out_stride_head, direction, stream),
+           "libra_rope_apply")
 
 
 def libra_rollout_dp(n_gpus: int, lengths, tp_set, cost_coef):
@@ -468,6 +508,15 @@ class Handle:
         _check(lib.libra_kv_scatter(self._h, k_dense_ptr, v_dense_ptr, block_table_ptr, seq_lens_ptr,
                                     token_offsets_ptr, batch, max_seq_len, head_begin, head_count, k_ptr, v_ptr,
                                     error_word_ptr, stream), "libra_kv_scatter")
+
+    def rope_append(self, rope: Rope | None, q_ptr: int, q_stride: int, q_out_ptr: int, q_out_stride: int, k_new_ptr: int,
+                    v_new_ptr: int, kv_stride: int, q_offsets_ptr: int, seq_lens_ptr: int, block_table_ptr: int,
+                    batch: int, max_rows: int, k_ptr: int, v_ptr: int, error_word_ptr: int, stream: int) -> None:
+        """Rotation of a packed batch of new q and k rows and append of k and v to the pages (rope None: no rotation;
+        q_ptr = q_out_ptr = 0: k and v only)."""
+        _check(lib.libra_rope_append(self._h, rope, q_ptr, q_stride, q_out_ptr, q_out_stride, k_new_ptr, v_new_ptr, kv_stride,
+                                     q_offsets_ptr, seq_lens_ptr, block_table_ptr, batch, max_rows, k_ptr, v_ptr,
+                                     error_word_ptr, stream), "libra_rope_append")
 
     def debug_wait_selftest(self, stream: int) -> None:
         _check(lib.libra_debug_wait_selftest(self._h, stream), "libra_debug_wait_selftest")

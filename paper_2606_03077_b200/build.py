@@ -6,8 +6,10 @@ library loads on machines without a driver (the planner entry point needs no GPU
 """
 from __future__ import annotations
 
+import concurrent.futures
 import hashlib
 import os
+import re
 import subprocess
 import sys
 
@@ -18,11 +20,13 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "liblibra.so")
 STAMP_PATH = os.path.join(HERE, "liblibra.so.stamp")
 
-SOURCES = ["libra_api.cu", "planner.cpp", "sched.cpp", "ring_sched.cpp"]
+SOURCES = ["libra_api.cu", "rope_api.cu", "planner.cpp", "sched.cpp", "ring_sched.cpp", "rope.cpp"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "--use_fast_math", "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+    "--use_fast_math", "-Xcompiler", "-fPIC",
 ]
+LINK_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static"]
+OBJ_DIR = os.path.join(HERE, "build")   # objects of the last build, kept so that only what changed is compiled again
 
 
 def _nvcc() -> str:
@@ -39,6 +43,27 @@ def _source_digest(extra_flags) -> str:
         path = n if os.path.isabs(n) else os.path.join(CSRC, n)
         with open(path, "rb") as f:
             h.update(n.encode() + b"\0" + f.read())
+    h.update(" ".join(SOURCES + NVCC_FLAGS + LINK_FLAGS + list(extra_flags)).encode())
+    return h.hexdigest()
+
+
+def _object_digest(source: str, extra_flags) -> str:
+    """Digest of one source and of every file of csrc / include that it includes, directly or not."""
+    h, todo, seen = hashlib.sha256(), [os.path.join(CSRC, source)], set()
+    while todo:
+        path = todo.pop()
+        if path in seen:
+            continue
+        seen.add(path)
+        with open(path, "rb") as f:
+            text = f.read()
+        h.update(os.path.basename(path).encode() + b"\0" + text)
+        for name in re.findall(rb'^\s*#\s*include\s+"([^"]+)"', text, flags=re.M):
+            for d in (CSRC, INCLUDE):
+                inc = os.path.join(d, name.decode())
+                if os.path.exists(inc):
+                    todo.append(inc)
+                    break
     h.update(" ".join(NVCC_FLAGS + list(extra_flags)).encode())
     return h.hexdigest()
 
@@ -50,14 +75,35 @@ def build_library(force: bool = False, verbose: bool = True, extra_flags=()) -> 
         with open(STAMP_PATH) as f:
             if f.read().strip() == digest:
                 return LIB_PATH
-    cmd = [_nvcc(), *NVCC_FLAGS, *extra_flags, "-I", INCLUDE, "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB_PATH]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-    if res.returncode != 0:
+    os.makedirs(OBJ_DIR, exist_ok=True)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        return subprocess.run(cmd, capture_output=True, text=True)
+
+    def compile_one(source):
+        obj = os.path.join(OBJ_DIR, source + ".o")
+        stamp, own = obj + ".stamp", _object_digest(source, extra_flags)
+        if not force and os.path.exists(obj) and os.path.exists(stamp):
+            with open(stamp) as f:
+                if f.read().strip() == own:
+                    return obj, None
+        res = run([_nvcc(), *NVCC_FLAGS, *extra_flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", obj])
+        if res.returncode == 0:
+            with open(stamp, "w") as f:
+                f.write(own)
+        return obj, res
+
+    with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, os.cpu_count() or 1)) as pool:
+        built = list(pool.map(compile_one, SOURCES))
+    results = [r for _, r in built if r is not None]
+    if all(r.returncode == 0 for r in results):
+        results.append(run([_nvcc(), *LINK_FLAGS, *[o for o, _ in built], "-o", LIB_PATH]))
+    failed = any(r.returncode != 0 for r in results)
+    if verbose or failed:
+        sys.stderr.write("".join(r.stdout + r.stderr for r in results))
+    if failed:
         raise RuntimeError("nvcc failed")
     with open(STAMP_PATH, "w") as f:
         f.write(digest)

@@ -1,0 +1,321 @@
+// Rotary positions: rotation of the channel pairs of every head by an angle that grows with the token's position.
+//
+//   pair i of a token at position p:  a = p theta_i ;  (x, y) -> m (x cos a - y sin a, x sin a + y cos a)
+//   gradient:                         the transposed map, the same with -a
+//
+// The angle is kept in turns as a 0.64 fixed-point number: p * (theta / 2 pi) modulo one turn is one 64-bit integer
+// product, exact for every position (a float32 product is wrong in the first digit at positions past 10^7).  What is
+// left after taking off whole quarter turns, at most an eighth of a turn, goes to sincospif.
+//
+// Both kernels below move every byte once and are bound by memory.  A block takes a few tokens: its threads compute the
+// tokens' sines and cosines once into shared memory (a token's pairs are the same for all of its heads: 64 evaluations
+// serve 16 KB of q and k) and then stream the heads, one item of V channels (half layout: V and V, `rotary_dim / 2`
+// apart) per thread and step.  V is 16 bytes' worth where pointers, strides and the rotated part allow it, else items
+// of one channel (half) or one pair (interleaved).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "libra.h"
+
+namespace libra {
+
+constexpr int kRopeThreads = 256;
+constexpr int kRopeMaxTokens = 8;   // tokens per block at most
+
+namespace rope {
+
+__device__ __forceinline__ float2 cos_sin(int32_t pos, uint64_t turns, float magnitude) {
+  const uint64_t phase = uint64_t(int64_t(pos)) * turns;   // modulo one turn
+  const int32_t t = int32_t(uint32_t(phase >> 32));        // signed, 2^-32 turns
+  const int32_t quarter = int32_t(uint32_t(t) + (1u << 29)) >> 30;   // nearest quarter turn (the sum wraps at half a turn)
+  const int32_t rest = int32_t(uint32_t(t) - (uint32_t(quarter) << 30));
+  float s, c;
+  sincospif(float(rest) * (1.0f / 2147483648.0f), &s, &c);   // |angle| <= pi / 4
+  const float cc = (quarter & 1) ? s : c, ss = (quarter & 1) ? c : s;
+  const float cr = ((quarter & 3) == 1 || (quarter & 3) == 2) ? -cc : cc;
+  const float sr = ((quarter & 3) >= 2) ? -ss : ss;
+  return make_float2(cr * magnitude, sr * magnitude);
+}
+
+template <typename T> __device__ __forceinline__ float to_f32(T x);
+template <> __device__ __forceinline__ float to_f32(float x) { return x; }
+template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <> __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_f32(float x) { return __float2half_rn(x); }
+
+// V elements of type T; 16 bytes at once when kVector
+template <typename T, int V, bool kVector>
+__device__ __forceinline__ void load(const T* p, T (&x)[V]) {
+  if constexpr (kVector) {
+    static_assert(sizeof(T) * V == 16, "one 16-byte vector");
+    *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = p[i];
+  }
+}
+template <typename T, int V, bool kVector>
+__device__ __forceinline__ void store(T* p, const T (&x)[V]) {
+  if constexpr (kVector) {
+    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = x[i];
+  }
+}
+
+// Items of one head: first those that rotate, then those that pass through.
+//   half         item j: channels [jV, jV + V) and the same R / 2 further on
+//   interleaved  item j: channels [jV, jV + V), V even
+template <int V, bool kHalf>
+__host__ __device__ __forceinline__ int rotating_items(int rotary_dim) {
+  return kHalf ? rotary_dim / (2 * V) : rotary_dim / V;
+}
+template <int V, bool kHalf>
+__host__ __device__ __forceinline__ int items_per_head(int rotary_dim, int head_dim) {
+  return rotating_items<V, kHalf>(rotary_dim) + (head_dim - rotary_dim) / V;
+}
+
+}  // namespace rope
+
+struct RopeApplyParams {
+  const void* x;
+  void* out;
+  const int32_t* positions;   // [tokens]
+  int64_t x_stride_token, x_stride_head, out_stride_token, out_stride_head;   // in elements
+  int64_t n_tokens;
+  int32_t n_heads, head_dim;
+  int32_t tokens_per_block;
+  int32_t gradient;
+  libra_rope_t rope;
+};
+
+// grid = ceil(tokens / tokens_per_block), block = kRopeThreads, dynamic shared memory = tokens_per_block * R / 2 float2
+template <typename T, int V, bool kVector, bool kHalf>
+__global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const __grid_constant__ RopeApplyParams p) {
+  extern __shared__ float2 cs[];   // [token][pair]
+  const int pairs = p.rope.rotary_dim / 2;
+  const int64_t t0 = int64_t(blockIdx.x) * p.tokens_per_block;
+  const int nt = int(p.n_tokens - t0 < p.tokens_per_block ? p.n_tokens - t0 : p.tokens_per_block);
+  for (int i = threadIdx.x; i < nt * pairs; i += kRopeThreads) {
+    const int tok = i / pairs, pr = i - tok * pairs;
+    float2 f = rope::cos_sin(__ldg(p.positions + t0 + tok), p.rope.turns[pr], p.rope.magnitude);
+    if (p.gradient) f.y = -f.y;
+    cs[i] = f;
+  }
+  __syncthreads();
+  const int rot = rope::rotating_items<V, kHalf>(p.rope.rotary_dim);
+  const int per_head = rope::items_per_head<V, kHalf>(p.rope.rotary_dim, p.head_dim);
+  const int per_token = per_head * p.n_heads;
+  const bool in_place = p.x == p.out;
+  for (int i = threadIdx.x; i < nt * per_token; i += kRopeThreads) {
+    const int tok = i / per_token, in_tok = i - tok * per_token;
+    const int head = in_tok / per_head, j = in_tok - head * per_head;
+    const T* src = static_cast<const T*>(p.x) + (t0 + tok) * p.x_stride_token + head * p.x_stride_head;
+    T* dst = static_cast<T*>(p.out) + (t0 + tok) * p.out_stride_token + head * p.out_stride_head;
+    alignas(16) T a[V];
+    if (j >= rot) {   // passes through
+      if (in_place) continue;
+      const int c = p.rope.rotary_dim + (j - rot) * V;
+      rope::load<T, V, kVector>(src + c, a);
+      rope::store<T, V, kVector>(dst + c, a);
+      continue;
+    }
+    const float2* f = cs + tok * pairs;
+    if constexpr (kHalf) {
+      alignas(16) T b[V];
+      rope::load<T, V, kVector>(src + j * V, a);
+      rope::load<T, V, kVector>(src + pairs + j * V, b);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float2 w = f[j * V + k];
+        const float x = rope::to_f32(a[k]), y = rope::to_f32(b[k]);
+        a[k] = rope::from_f32<T>(x * w.x - y * w.y);
+        b[k] = rope::from_f32<T>(x * w.y + y * w.x);
+      }
+      rope::store<T, V, kVector>(dst + j * V, a);
+      rope::store<T, V, kVector>(dst + pairs + j * V, b);
+    } else {
+      rope::load<T, V, kVector>(src + j * V, a);
+#pragma unroll
+      for (int k = 0; k < V; k += 2) {
+        const float2 w = f[(j * V + k) / 2];
+        const float x = rope::to_f32(a[k]), y = rope::to_f32(a[k + 1]);
+        a[k] = rope::from_f32<T>(x * w.x - y * w.y);
+        a[k + 1] = rope::from_f32<T>(x * w.y + y * w.x);
+      }
+      rope::store<T, V, kVector>(dst + j * V, a);
+    }
+  }
+}
+
+struct RopeAppendParams {
+  const __nv_bfloat16* q;      // or null: nothing is rotated but k
+  __nv_bfloat16* q_out;
+  const __nv_bfloat16* k_new;
+  const __nv_bfloat16* v_new;
+  int64_t q_stride, q_out_stride, kv_stride;   // elements from a token to the next
+  const int32_t* q_offsets;    // [batch + 1]
+  const int32_t* seq_lens;     // [batch]
+  const int32_t* block_table;  // [batch][ld]
+  void* k_pool;
+  void* v_pool;
+  uint32_t* error_word;
+  int64_t stride_page, stride_head, stride_token;   // pool strides in elements
+  int64_t num_pages;
+  float k_inv_scale, v_inv_scale;                   // E4M3 pools
+  int32_t batch, max_tokens;
+  int32_t block_table_ld, page_shift;
+  int32_t num_q_heads, num_kv_heads, head_dim;
+  int32_t tokens_per_block;
+  libra_rope_t rope;
+};
+
+namespace rope {
+
+// V float32 values into the pool's element type.
+template <typename P, int V, bool kVector>
+__device__ __forceinline__ void store_pool(P* dst, const float (&x)[V], float inv_scale) {
+  if constexpr (sizeof(P) == 2) {
+    alignas(16) __nv_bfloat16 y[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) y[k] = __float2bfloat16_rn(x[k]);
+    store<__nv_bfloat16, V, kVector>(reinterpret_cast<__nv_bfloat16*>(dst), y);
+  } else {   // E4M3: round to nearest even, beyond the largest code = the largest code
+    alignas(8) uint8_t y[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) y[k] = __nv_cvt_float_to_fp8(x[k] * inv_scale, __NV_SATFINITE, __NV_E4M3);
+    if constexpr (kVector) {
+      *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(y);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) reinterpret_cast<uint8_t*>(dst)[k] = y[k];
+    }
+  }
+}
+
+}  // namespace rope
+
+// Rotation of q and k of a ragged batch of new tokens and append of k and v to the pages.
+// P: element of the pools (__nv_bfloat16 or uint8_t = E4M3 code).
+// grid = ceil(max_tokens / tokens_per_block), block = kRopeThreads, dynamic shared memory as above.
+template <typename P, int V, bool kVector, bool kHalf>
+__global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_constant__ RopeAppendParams p) {
+  extern __shared__ float2 cs[];              // [token][pair]
+  __shared__ int32_t s_pos[kRopeMaxTokens];
+  __shared__ int64_t s_slot[kRopeMaxTokens];  // pool offset of the token's slot, head 0; -1: not stored; -2: no token
+  const int pairs = p.rope.rotary_dim / 2;
+  const int t0 = blockIdx.x * p.tokens_per_block;
+  const int nt = min(p.tokens_per_block, p.max_tokens - t0);
+  if (threadIdx.x < nt) {
+    const int row = t0 + threadIdx.x;
+    // the last sequence whose rows begin at or before this one (sequences without new tokens share a beginning)
+    int lo = 0, hi = p.batch;   // q_offsets[lo] <= row < q_offsets[hi], if the row belongs to anyone
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (__ldg(p.q_offsets + mid) <= row) lo = mid;
+      else hi = mid;
+    }
+    int64_t slot = -2;
+    int32_t pos = 0;
+    const int32_t first = __ldg(p.q_offsets + lo), end = __ldg(p.q_offsets + lo + 1);
+    if (row >= first && row < end) {
+      pos = __ldg(p.seq_lens + lo) - end + row;
+      slot = -1;
+      const int page_index = pos >> p.page_shift;
+      if (pos >= 0 && page_index >= p.block_table_ld) {
+        atomicOr(p.error_word, uint32_t(LIBRA_ERR_PLAN_OVERFLOW));
+      } else if (pos >= 0) {
+        const int64_t page = __ldg(p.block_table + int64_t(lo) * p.block_table_ld + page_index);
+        if (page < 0 || page >= p.num_pages) {
+          atomicOr(p.error_word, uint32_t(LIBRA_ERR_BAD_PAGE_ID));
+        } else {
+          slot = page * p.stride_page + int64_t(pos & ((1 << p.page_shift) - 1)) * p.stride_token;
+        }
+      }
+    }
+    s_pos[threadIdx.x] = pos;
+    s_slot[threadIdx.x] = slot;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < nt * pairs; i += kRopeThreads) {
+    const int tok = i / pairs, pr = i - tok * pairs;
+    cs[i] = rope::cos_sin(s_pos[tok], p.rope.turns[pr], p.rope.magnitude);
+  }
+  __syncthreads();
+  const int rot = rope::rotating_items<V, kHalf>(p.rope.rotary_dim);
+  const int per_head = rope::items_per_head<V, kHalf>(p.rope.rotary_dim, p.head_dim);
+  const int v_per_head = p.head_dim / V;
+  const int q_heads = p.q ? p.num_q_heads : 0;
+  const int qk_items = (q_heads + p.num_kv_heads) * per_head;
+  const int per_token = qk_items + p.num_kv_heads * v_per_head;
+  for (int i = threadIdx.x; i < nt * per_token; i += kRopeThreads) {
+    const int tok = i / per_token, in_tok = i - tok * per_token;
+    const int64_t row = t0 + tok, slot = s_slot[tok];
+    if (slot == -2) continue;   // a row behind the last sequence
+    alignas(16) __nv_bfloat16 a[V];
+    float x[V];
+    if (in_tok >= qk_items) {   // a value row: copied
+      if (slot < 0) continue;
+      const int head = (in_tok - qk_items) / v_per_head, c = (in_tok - qk_items - head * v_per_head) * V;
+      rope::load<__nv_bfloat16, V, kVector>(p.v_new + row * p.kv_stride + head * p.head_dim + c, a);
+#pragma unroll
+      for (int k = 0; k < V; ++k) x[k] = __bfloat162float(a[k]);
+      rope::store_pool<P, V, kVector>(static_cast<P*>(p.v_pool) + slot + head * p.stride_head + c, x, p.v_inv_scale);
+      continue;
+    }
+    const int head = in_tok / per_head, j = in_tok - head * per_head;
+    const bool is_q = head < q_heads;
+    if (!is_q && slot < 0) continue;
+    const __nv_bfloat16* src = is_q ? p.q + row * p.q_stride + head * p.head_dim
+                                    : p.k_new + row * p.kv_stride + (head - q_heads) * p.head_dim;
+    __nv_bfloat16* q_dst = p.q_out + row * p.q_out_stride + head * p.head_dim;                                   // if is_q
+    P* k_dst = static_cast<P*>(p.k_pool) + slot + (head - q_heads) * p.stride_head;                              // else
+    auto put = [&](int c, const float (&y)[V]) {
+      if (is_q) rope::store_pool<__nv_bfloat16, V, kVector>(q_dst + c, y, 1.f);
+      else rope::store_pool<P, V, kVector>(k_dst + c, y, p.k_inv_scale);
+    };
+    const float2* f = cs + tok * pairs;
+    if (j >= rot) {
+      const int c = p.rope.rotary_dim + (j - rot) * V;
+      rope::load<__nv_bfloat16, V, kVector>(src + c, a);
+#pragma unroll
+      for (int k = 0; k < V; ++k) x[k] = __bfloat162float(a[k]);
+      put(c, x);
+    } else if constexpr (kHalf) {
+      alignas(16) __nv_bfloat16 b[V];
+      float y[V];
+      rope::load<__nv_bfloat16, V, kVector>(src + j * V, a);
+      rope::load<__nv_bfloat16, V, kVector>(src + pairs + j * V, b);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float2 w = f[j * V + k];
+        const float u = __bfloat162float(a[k]), v = __bfloat162float(b[k]);
+        x[k] = u * w.x - v * w.y;
+        y[k] = u * w.y + v * w.x;
+      }
+      put(j * V, x);
+      put(pairs + j * V, y);
+    } else {
+      rope::load<__nv_bfloat16, V, kVector>(src + j * V, a);
+#pragma unroll
+      for (int k = 0; k < V; k += 2) {
+        const float2 w = f[(j * V + k) / 2];
+        const float u = __bfloat162float(a[k]), v = __bfloat162float(a[k + 1]);
+        x[k] = u * w.x - v * w.y;
+        x[k + 1] = u * w.y + v * w.x;
+      }
+      put(j * V, x);
+    }
+  }
+}
+
+}  // namespace libra
