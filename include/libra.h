@@ -70,6 +70,8 @@ typedef enum {
 #define LIBRA_ERR_SEQ_LEN_MISMATCH 4u /* device seq_lens differ from the lengths that were planned */
 #define LIBRA_ERR_PLAN_OVERFLOW 8u  /* device-side planner: too many sequences or work items, or a length
                                        longer than a block-table row can describe; nothing was computed */
+#define LIBRA_ERR_PLAN_CHANGED 16u  /* chunk attention: the workspace no longer holds the plan that the launch was made
+                                       for (a recorded launch replayed after another plan); nothing was computed     */
 
 /* Planner constants (Section 4.3 of the paper: degrees are powers of two, work sorted by length,
  * min-max objective).  A zero field takes its default. */
@@ -448,7 +450,8 @@ int libra_kv_scatter(libra_handle_t handle, const void* k_dense, const void* v_d
 /* ---- Chunks of new tokens: rotary positions, append to the pages, attention over them --------------------------------
  * A trajectory grows by more than a token at a time when it starts (its prompt) and at every tool return (Section 2.2
  * of the paper).  The calls below absorb such chunks: libra_rope_append rotates the new tokens' q and k and writes k and v
- * into the pages.  The new tokens of a batch are packed: those of sequence b are rows
+ * into the pages, libra_chunk_attn then runs causal attention of the new tokens over the pages; single tokens
+ * afterwards go through libra_decode_attn.  The new tokens of a batch are packed: those of sequence b are rows
  * q_offsets[b] .. q_offsets[b + 1] - 1 of q, in order, and seq_lens[b] counts them, so that row q_offsets[b] + i is token
  * seq_lens[b] - q_len_b + i of its sequence (q_len_b = q_offsets[b + 1] - q_offsets[b]; 0 is allowed). */
 
@@ -531,6 +534,49 @@ int libra_rope_append(libra_handle_t handle, const libra_rope_t* rope, const voi
                       int64_t q_out_stride, const void* k_new, const void* v_new, int64_t kv_stride,
                       const int32_t* q_offsets, const int32_t* seq_lens, const int32_t* block_table, int32_t batch,
                       int32_t max_rows, void* k_pages, void* v_pages, void* error_word_dev, void* stream);
+
+/* Plan of the chunk attention, a pure host function (needs no GPU).  A chunk's query rows are flattened per KV head (row
+ * r = query token r / G, head r % G of the group) and cut into tiles of 256 rows; where that gives too few blocks to fill
+ * n_sm multiprocessors, the KV ranges are cut too, into equal runs of 128-token steps.  items: 8 int32 each, longest first:
+ *   {b, first row of sequence b in q, first flattened row, rows, kv_begin, kv_end, seq_len - q_len, slot}
+ * slot < 0: the range is whole.  merges: 8 int32 per cut tile: {first row of the sequence, first flattened row, rows, slot
+ * of its first chunk, chunks, 0, 0, 0}; chunk j's partial rows begin at slot + j * rows; *partial_rows counts them.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (more than 2^31 - 1 rows), WORKSPACE_TOO_SMALL (a capacity, in items, is too
+ * small; *num_items and *num_merges hold what is needed). */
+int libra_chunk_plan_host(int32_t n_sm, int32_t num_q_heads, int32_t num_kv_heads, const int32_t* q_lens,
+                          const int32_t* seq_lens, int32_t batch, int32_t* items, int32_t items_capacity,
+                          int32_t* num_items, int32_t* merges, int32_t merges_capacity, int32_t* num_merges,
+                          int64_t* partial_rows);
+
+/* Bytes of device workspace that libra_chunk_plan / libra_chunk_attn need for any batch of at most max_batch sequences with at
+ * most max_tokens new tokens together (256-byte aligned; not the workspace of libra_plan). */
+int libra_chunk_workspace_size(libra_handle_t handle, int64_t max_tokens, size_t* bytes);
+
+/* Plan a batch for libra_chunk_attn from host lengths (int32[batch] each) and enqueue the plan's copy into the workspace on
+ * `stream`.  One plan serves any number of libra_chunk_attn calls on the same lengths (the layers of a model).  Independent of
+ * libra_plan: a handle holds one plan of each kind.  Not while `stream` is being recorded (INVALID_ARGUMENT): the copy's source is
+ * a buffer of the handle.  Errors: INVALID_ARGUMENT (also: a length that a block-table row cannot describe),
+ * UNSUPPORTED_SHAPE, WORKSPACE_TOO_SMALL, CUDA_ERROR. */
+int libra_chunk_plan(libra_handle_t handle, const int32_t* q_lens_host, const int32_t* seq_lens_host, int32_t batch,
+                     void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Causal attention of the planned chunks over the pages:  for row r = q_offsets[b] + i and query head h,
+ *     out[r, h] = softmax over cached tokens t = 0 .. seq_len_b - q_len_b + i of (q[r, h] . K_b[t]) * sm_scale, times V
+ * with the handle's geometry, pool type and scale, exactly as libra_decode_attn defines them; a row with nothing to attend to
+ * (seq_len_b - q_len_b + i < 0) gets zeros.  q: bf16, row r at r * q_stride elements (>= num_q_heads * head_dim, a multiple
+ * of 8), 16-byte aligned; out: bf16 [rows, num_q_heads, head_dim], 16-byte aligned, not overlapping q; lse: float32 [rows,
+ * num_q_heads] or NULL, natural logarithm, -inf for a row that sees nothing.  The K and V of all tokens, the new ones
+ * included, are already in the pages.  Slots past a sequence's end and unowned pages never influence a result; a value that is
+ * not finite in a slot that a sequence owns may reach every new row of that sequence and KV head, earlier ones too.
+ * Probabilities are rounded to 16 bits for the tensor cores (bf16; fp16 over E4M3 pools), everything else is float32.
+ * Results are bit-reproducible run to run.  Bits of *error_word_dev: LIBRA_ERR_BAD_PAGE_ID (such a page reads as zeros),
+ * LIBRA_ERR_WAIT_TIMEOUT, LIBRA_ERR_PLAN_CHANGED.
+ * The launch may be recorded in a CUDA graph: a replay uses the plan in the workspace, which therefore has to stay (if another
+ * plan was put there the replay computes nothing and says so in the error word), and the partial results in it, so two
+ * graphs whose replays can overlap need a workspace each.  Asynchronous on `stream`.
+ * Errors: INVALID_ARGUMENT, NOT_PLANNED, CUDA_ERROR. */
+int libra_chunk_attn(libra_handle_t handle, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
+                     const int32_t* block_table, void* out, float* lse, void* error_word_dev, void* stream);
 
 /* ---- the paper's rollout-side schedulers, host code only (no GPU) ------------------------------------ */
 

@@ -22,7 +22,7 @@ STATIC_SCRATCH_BYTES = 8 << 20
 OK, INVALID_ARGUMENT, UNSUPPORTED_SHAPE, WORKSPACE_TOO_SMALL, NOT_PLANNED, CUDA_ERROR, DEVICE_FLAGGED = range(7)
 KV_BF16, KV_E4M3 = 0, 1
 RING_F32, RING_BF16 = 0, 1
-ERR_WAIT_TIMEOUT, ERR_BAD_PAGE_ID, ERR_SEQ_LEN_MISMATCH, ERR_PLAN_OVERFLOW = 1, 2, 4, 8
+ERR_WAIT_TIMEOUT, ERR_BAD_PAGE_ID, ERR_SEQ_LEN_MISMATCH, ERR_PLAN_OVERFLOW, ERR_PLAN_CHANGED = 1, 2, 4, 8, 16
 
 
 class PlanParams(C.Structure):
@@ -141,6 +141,11 @@ SIGNATURES = {
                                    C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, _vp]),
     "libra_rope_append": (C.c_int, [_vp, C.POINTER(Rope), _vp, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, _vp,
                                     C.c_int32, C.c_int32, _vp, _vp, _vp, _vp]),
+    "libra_chunk_plan_host": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, _i32p, _i32p, C.c_int32, _i32p, C.c_int32, _i32p, _i32p,
+                                        C.c_int32, _i32p, C.POINTER(C.c_int64)]),
+    "libra_chunk_workspace_size": (C.c_int, [_vp, C.c_int64, C.POINTER(C.c_size_t)]),
+    "libra_chunk_plan": (C.c_int, [_vp, _i32p, _i32p, C.c_int32, _vp, C.c_size_t, _vp]),
+    "libra_chunk_attn": (C.c_int, [_vp, _vp, C.c_int64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "libra_rollout_dp": (C.c_int, [C.c_int32, _i32p, C.c_int32, _i32p, C.c_int32, C.POINTER(C.c_double),
                                    C.POINTER(C.c_double), _i32p, _i32p, _i32p, C.c_int32, _i32p]),
     "libra_trie_create": (C.c_int, [C.POINTER(_vp), _i32p, C.c_int32]),
@@ -279,6 +284,22 @@ def libra_rope_apply(device: int, rope: Rope, x_ptr: int, out_ptr: int, dtype: i
     _check(lib.libra_rope_apply(device, rope, x_ptr, out_ptr, dtype, positions_ptr, n_tokens, n_heads, head_dim,
                                 x_stride_token, x_stride_head, out_stride_token, out_stride_head, direction, stream),
            "libra_rope_apply")
+
+
+def libra_chunk_plan_host(n_sm: int, num_q_heads: int, num_kv_heads: int, q_lens, seq_lens) -> dict:
+    """Plan of the chunk attention as NumPy arrays: items [n, 8], merges [m, 8], and the number of partial rows."""
+    ql, sl = _as_i32(q_lens), _as_i32(seq_lens)
+    n, m, rows = C.c_int32(0), C.c_int32(0), C.c_int64(0)
+    p = lambda a: a.ctypes.data_as(_i32p)
+    call = lambda items, merges: lib.libra_chunk_plan_host(n_sm, num_q_heads, num_kv_heads, p(ql), p(sl), len(ql), p(items),
+                                                           len(items), C.byref(n), p(merges), len(merges), C.byref(m), C.byref(rows))
+    items, merges = (np.zeros((0, 8), np.int32) for _ in range(2))
+    st = call(items, merges)
+    if st == WORKSPACE_TOO_SMALL:
+        items, merges = np.zeros((n.value, 8), np.int32), np.zeros((m.value, 8), np.int32)
+        st = call(items, merges)
+    _check(st, "libra_chunk_plan_host")
+    return {"items": items, "merges": merges, "partial_rows": rows.value}
 
 
 def libra_rollout_dp(n_gpus: int, lengths, tp_set, cost_coef):
@@ -517,6 +538,25 @@ class Handle:
         _check(lib.libra_rope_append(self._h, rope, q_ptr, q_stride, q_out_ptr, q_out_stride, k_new_ptr, v_new_ptr, kv_stride,
                                      q_offsets_ptr, seq_lens_ptr, block_table_ptr, batch, max_rows, k_ptr, v_ptr,
                                      error_word_ptr, stream), "libra_rope_append")
+
+    def chunk_workspace_size(self, max_tokens: int) -> int:
+        n = C.c_size_t(0)
+        _check(lib.libra_chunk_workspace_size(self._h, max_tokens, C.byref(n)), "libra_chunk_workspace_size")
+        return n.value
+
+    def chunk_plan(self, q_lens_host: np.ndarray, seq_lens_host: np.ndarray, workspace_ptr: int, workspace_bytes: int,
+                   stream: int) -> None:
+        ql, sl = _as_i32(q_lens_host), _as_i32(seq_lens_host)
+        if ql.shape != sl.shape:
+            raise ValueError("q_lens and seq_lens are of one batch")
+        _check(lib.libra_chunk_plan(self._h, ql.ctypes.data_as(_i32p), sl.ctypes.data_as(_i32p), int(ql.shape[0]), workspace_ptr,
+                                    workspace_bytes, stream), "libra_chunk_plan")
+
+    def chunk_attn(self, q_ptr: int, q_stride: int, k_ptr: int, v_ptr: int, block_table_ptr: int, out_ptr: int, lse_ptr: int,
+                   error_word_ptr: int, stream: int) -> None:
+        """Causal attention of the planned chunks of new tokens over the pages (lse_ptr 0: not wanted)."""
+        _check(lib.libra_chunk_attn(self._h, q_ptr, q_stride, k_ptr, v_ptr, block_table_ptr, out_ptr, lse_ptr or None,
+                                    error_word_ptr, stream), "libra_chunk_attn")
 
     def debug_wait_selftest(self, stream: int) -> None:
         _check(lib.libra_debug_wait_selftest(self._h, stream), "libra_debug_wait_selftest")

@@ -1,0 +1,809 @@
+// Causal attention of packed chunks of new tokens over the paged KV cache (sm_100a).
+//
+// For one item (up to 256 flattened query rows of one sequence and KV head, row = query token x head of the group) and a
+// range of cached tokens, in steps of 128 tokens:
+//
+//   S = Q K^T          tcgen05.mma, Q and K tiles in shared memory, S (128 x 128 fp32) in tensor memory
+//   P = 2^(S c - m c)  in registers, one row per thread; rounded to 16 bits and put where S was
+//   O += P V           tcgen05.mma, P from tensor memory, V tile in shared memory, O (128 x D fp32) in tensor memory
+//
+// with the running maximum m and sum l of an online softmax.  m is raised, and O and l scaled, only when a tile's maximum
+// exceeds it by more than 2^8 (the probabilities then lie below 2^8 instead of 1, which 16-bit and fp32 numbers hold as
+// well), so that O stays untouched in tensor memory for most steps.
+//
+// Roles of a block's warps: 0-3 and 4-7 softmax of row tiles 0 and 1 (and loading Q, writing the output), 8 the copies, 9 the
+// tensor-core instructions; over an E4M3 cache 12-15 convert K and V.  While one tile's rows are in the softmax the tensor
+// cores work on the other's.  An item of at most 128 rows has one row tile: then both softmax groups take it, one the even
+// steps and one the odd ones, and their results are merged in shared memory at the end.
+//
+// Copies: one tiled TMA load per page (16, 32 or 64 tokens) and 64 channels, 128-byte swizzle, into a ring of tiles.  Pages
+// past the range are not read; what their rows of V hold is overwritten with zeros (0 x NaN would reach the result), scores
+// past a row's limit are set to -inf by selection.
+//
+// E4M3 cache: the codes arrive as bytes and are converted to fp16 (exact).  q goes to fp16 too, every row multiplied by a
+// power of two that brings its largest element to 2^10 .. 2^11: elements 2^-25 below it and larger stay exact, the rest lose
+// less than a float32 product would.  P is rounded to fp16.
+//
+// Every wait is bounded; the first one that runs out sets the block's stop flag and the error word, and every role leaves.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "chunk_plan.hpp"
+#include "libra.h"
+#include "ptx.cuh"
+
+namespace libra {
+
+struct ChunkParams {
+  const __nv_bfloat16* q;
+  int64_t q_stride;
+  const int32_t* block_table;
+  __nv_bfloat16* out;
+  float* lse;                 // or null
+  const uint32_t* serial_at;  // the plan in the workspace: its serial number, its items
+  const int4* items;
+  float* partial_o;           // [partial row][KV head][D]
+  float* partial_lse;         // [partial row][KV head]
+  uint32_t* error_word;
+  int64_t num_pages;
+  uint32_t serial;
+  int32_t num_units;          // items x KV heads
+  int32_t num_q_heads, num_kv_heads, group;
+  int32_t block_table_ld;
+  int32_t page_shift;
+  int32_t pos_head, pos_page, pos_token;
+  float scale_log2;           // sm_scale * log2(e) * k_scale
+  float v_scale;
+};
+
+template <int D, bool kFp8>
+struct ChunkShape {
+  static constexpr int kTileBytes = kChunkKvTile * D * 2;      // a tile of K or V (and of Q) as the tensor cores read it
+  static constexpr int kRawBytes = kChunkKvTile * D;           // the same as E4M3 codes
+  static constexpr int kStages = kFp8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);
+  static constexpr int kRawStages = kFp8 ? (D == 128 ? 4 : 8) : 0;
+  static constexpr int kThreads = kFp8 ? 512 : 384;
+  // dynamic shared memory: Q tiles | ring | raw ring | floats | barriers
+  static constexpr int kRing = 2 * kTileBytes;
+  static constexpr int kRaw = kRing + kStages * kTileBytes;
+  static constexpr int kFloats = kRaw + kRawStages * kRawBytes;   // 2 x 128 row factors, 2 x 128 (m, l) of the merge
+  static constexpr int kBars = kFloats + 4 * 128 * 4;
+  static constexpr int kDynamicBytes = kBars + 512;
+  static_assert(kDynamicBytes <= 227 * 1024, "shared memory of a block");
+};
+
+namespace chunk {
+
+using namespace dev;
+
+// barriers, in 8-byte slots after the floats
+constexpr int kBarFull = 0, kBarEmpty = 8, kBarRawFull = 16, kBarRawEmpty = 24, kBarQ = 32, kBarS = 34, kBarP = 36, kBarO = 38,
+              kBarMergeFree = 40, kBarMergeFull = 41, kBarMergeDone = 42, kBarTail = 43, kBarDrain = 44;
+constexpr int kSlotStop = 46, kSlotTmem = 47;   // the stop flag and the tensor-memory address live in two more slots
+
+struct Stop {   // how a wait that ran out ends the block
+  volatile uint32_t* flag;
+  uint32_t* error_word;
+};
+
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, const Stop& stop) {
+  if (mbar_try_wait(bar, parity)) return true;
+  for (uint32_t i = 0; i < kWaitLimit; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (*stop.flag) return false;
+  }
+  *stop.flag = 1;
+  atomicOr(stop.error_word, uint32_t(LIBRA_ERR_WAIT_TIMEOUT));
+  return false;
+}
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const Stop& stop) {
+  return __all_sync(0xffffffffu, wait(bar, parity, stop));
+}
+__device__ __forceinline__ void arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// ---- tensor memory and tensor-core instructions
+__device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t columns) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_dealloc(uint32_t addr, uint32_t columns) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 32 columns of this warp's 32 lanes: register i of a thread is column i of its lane
+__device__ __forceinline__ void tmem_ld(float* r, uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+        "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]),
+        "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]),
+        "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+      : "r"(addr));
+}
+// Uses of these registers come after the wait that precedes this in the program.
+__device__ __forceinline__ void settle(float* r) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(r[i]));
+}
+__device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(
+          addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+      "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+      "r"(r[31])
+      : "memory");
+}
+
+// Shared-memory matrix descriptor, 128-byte swizzle.  K-major tiles (Q, K: channels contiguous): `sbo` is the distance of
+// 8-row groups and `lbo` is not read.  MN-major tiles (V: the channels are the N of the product): `lbo` is the distance of
+// 64-channel groups, `sbo` that of 8-token groups.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+  return uint64_t((addr >> 4) & 0x3fff) | (uint64_t(lbo >> 4) << 16) | (uint64_t(sbo >> 4) << 32) | (uint64_t(1) << 46) |
+         (uint64_t(2) << 61);
+}
+// Instruction descriptor: fp32 accumulation, 16-bit operands (bf16 or fp16), M = 128
+template <bool kBf16>
+__host__ __device__ constexpr uint32_t instr_desc(int n, bool b_mn_major) {
+  return (1u << 4) | (kBf16 ? (1u << 7) | (1u << 10) : 0u) | (b_mn_major ? 1u << 16 : 0u) | (uint32_t(n >> 3) << 17) |
+         (uint32_t(kChunkTileRows >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
+      : "memory");
+}
+// Completes on `bar` once everything this thread has issued to the tensor cores is done.
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  uint32_t d;
+  if constexpr (kBf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
+// Byte offset of 16-byte chunk c16 of row r in a tile of 128 rows: [D / 64][128 rows][128 bytes], 128-byte swizzle
+__device__ __forceinline__ uint32_t swizzled(int r, int c16) {
+  return uint32_t(((c16 >> 3) << 14) + (r << 7) + (((c16 & 7) ^ (r & 7)) << 4));
+}
+__device__ __forceinline__ void st_shared(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// Eight bf16 of a row that kLanes neighbouring lanes hold -> fp16, the row multiplied by the power of two that brings its
+// largest element to 2^10 .. 2^11; `down` undoes it.
+template <int kLanes>
+__device__ __forceinline__ uint4 scaled_half_row(uint4 v, float& down) {
+  float f[8];
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    most = fmaxf(most, fmaxf(fabsf(f[2 * i]), fabsf(f[2 * i + 1])));
+  }
+#pragma unroll
+  for (int off = kLanes / 2; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+  // exponent of the largest element, kept where both factors are normal numbers; not finite: as it is
+  const int e = max(int((__float_as_uint(most) >> 23) & 255) - 127, -107);
+  const float up = e == 128 ? 1.f : __uint_as_float(uint32_t(127 + 10 - e) << 23);
+  down = e == 128 ? 1.f : __uint_as_float(uint32_t(127 - 10 + e) << 23);
+  uint32_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = pack<false>(f[2 * i] * up, f[2 * i + 1] * up);
+  return make_uint4(h[0], h[1], h[2], h[3]);
+}
+
+// One unit of work as every role sees it.
+struct ChunkUnit {
+  int b, q_start, row0, n_rows, kv_begin, kv_end, ctx, slot;
+  int head;    // KV head
+  int steps;   // of 128 cached tokens
+  bool solo;   // one row tile, the softmax groups take turns on the steps
+  // steps of row tile (softmax group) t
+  __device__ __forceinline__ int steps_of(int t) const { return solo ? (steps + 1 - t) >> 1 : steps; }
+};
+__device__ __forceinline__ ChunkUnit load_unit(const ChunkParams& p, int u) {
+  const int4 a = __ldg(p.items + 2 * (u / p.num_kv_heads)), c = __ldg(p.items + 2 * (u / p.num_kv_heads) + 1);
+  ChunkUnit x;
+  x.b = a.x; x.q_start = a.y; x.row0 = a.z; x.n_rows = a.w;
+  x.kv_begin = c.x; x.kv_end = c.y; x.ctx = c.z; x.slot = c.w;
+  x.head = u % p.num_kv_heads;
+  x.steps = (x.kv_end - x.kv_begin + kChunkKvTile - 1) / kChunkKvTile;
+  x.solo = x.n_rows <= kChunkTileRows;
+  return x;
+}
+
+}  // namespace chunk
+
+template <int D, bool kFp8>
+__global__ void __launch_bounds__(ChunkShape<D, kFp8>::kThreads, 1)
+chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+             const __grid_constant__ ChunkParams p) {
+  using namespace chunk;
+  using Shape = ChunkShape<D, kFp8>;
+  constexpr bool kBf16 = !kFp8;
+  constexpr int kStages = Shape::kStages;
+  constexpr uint32_t kTmemColumns = 512;                  // S0 | S1 | O0 | O1, 128 columns each (O: D of them)
+  extern __shared__ __align__(1024) uint8_t smem[];   // the 128-byte swizzle counts rows from 1024-byte boundaries
+  const uint32_t base = smem_u32(smem);
+  const uint32_t q_tiles = base, ring = base + Shape::kRing, raw = base + Shape::kRaw;
+  float* const row_factor = reinterpret_cast<float*>(smem + Shape::kFloats);   // [2][128]
+  float* const merge_ml = row_factor + 256;                                    // [2][128]
+  auto bar = [&](int i) { return base + uint32_t(Shape::kBars + 8 * i); };
+  volatile uint32_t* const slots = reinterpret_cast<volatile uint32_t*>(smem + Shape::kBars);
+  Stop stop{slots + 2 * kSlotStop, p.error_word};
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(bar(kBarFull + s), kFp8 ? 128 : 1);
+      mbar_init(bar(kBarEmpty + s), 1);
+    }
+    for (int s = 0; s < Shape::kRawStages; ++s) {
+      mbar_init(bar(kBarRawFull + s), 1);
+      mbar_init(bar(kBarRawEmpty + s), 128);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(bar(kBarQ + t), 128);
+      mbar_init(bar(kBarS + t), 1);
+      mbar_init(bar(kBarP + t), 128);
+      mbar_init(bar(kBarO + t), 1);
+    }
+    mbar_init(bar(kBarMergeFree), 128);
+    mbar_init(bar(kBarMergeFull), 128);
+    mbar_init(bar(kBarMergeDone), 128);
+    mbar_init(bar(kBarTail), 1);
+    mbar_init(bar(kBarDrain), 1);
+    fence_mbar_init();
+    // another plan in the workspace than the one this launch was made for: nothing is computed
+    const uint32_t found = *reinterpret_cast<const volatile uint32_t*>(p.serial_at);
+    slots[2 * kSlotStop] = (found != p.serial || (base & 1023u) != 0) ? 1u : 0u;
+    if (found != p.serial) atomicOr(p.error_word, uint32_t(LIBRA_ERR_PLAN_CHANGED));
+  }
+  if (warp == 9) tmem_alloc(bar(kSlotTmem), kTmemColumns);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = slots[2 * kSlotTmem];
+  const bool run = slots[2 * kSlotStop] == 0;
+  __syncthreads();   // every thread has read the stop flag before a role can set it
+
+  if (run && warp < 8) {
+    // ------------------------------------------------------------------ softmax group t: row tile t (both: tile 0 if solo)
+    if constexpr (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    const int t = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    const uint32_t s_tmem = tmem + lanes + t * 128, o_tmem = tmem + lanes + 256 + t * 128;
+    uint32_t n_s = 0, n_q = 0, n_o = 0, n_solo = 0;   // phases seen
+    for (int u = blockIdx.x; u < p.num_units; u += gridDim.x) {
+      const ChunkUnit x = load_unit(p, u);
+      const int steps = x.steps_of(t);
+      const int tile_row = (x.solo ? 0 : t * kChunkTileRows) + row;   // row within the item
+      const bool valid = tile_row < x.n_rows;
+      const int token = (x.row0 + (valid ? tile_row : 0)) / p.group;
+      const int q_head = x.head * p.group + (x.row0 + (valid ? tile_row : 0)) - token * p.group;
+      // ---- Q: 16 lanes (8 at D = 64) bring one row
+      if (x.steps > 0 && !(x.solo && t == 1)) {
+        constexpr int kLanes = D / 8, kRowsAtOnce = 128 / kLanes, kBatch = 8;
+        const int c16 = row % kLanes;
+#pragma unroll 1
+        for (int r0 = row / kLanes; r0 < kChunkTileRows; r0 += kRowsAtOnce * kBatch) {
+          uint4 v[kBatch];
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int ir = t * kChunkTileRows + r0 + i * kRowsAtOnce;
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (ir < x.n_rows) {
+              const int flat = x.row0 + ir, tok = flat / p.group;
+              v[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (int64_t(x.q_start) + tok) * p.q_stride +
+                                                          int64_t(x.head * p.group + flat - tok * p.group) * D) + c16);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int r = r0 + i * kRowsAtOnce;
+            if constexpr (kFp8) {
+              float down;
+              v[i] = scaled_half_row<kLanes>(v[i], down);
+              if (c16 == 0) row_factor[t * 128 + r] = down;
+            }
+            st_shared(q_tiles + t * Shape::kTileBytes + swizzled(r, c16), v[i]);
+          }
+        }
+      }
+      fence_proxy_async();
+      arrive(bar(kBarQ + t));
+      if constexpr (kFp8) {
+        // the row factors come from the group that loaded the tile
+        if (!wait_warp(bar(kBarQ + (x.solo ? 0 : t)), n_q & 1, stop)) break;
+      }
+      ++n_q;
+      float rs = p.scale_log2;   // score -> base-2 exponent
+      if constexpr (kFp8) {
+        if (x.steps > 0) rs *= row_factor[(x.solo ? 0 : t) * 128 + row];
+      }
+      // ---- the steps
+      const int sees = valid ? min(x.kv_end, x.ctx + token + 1) : 0;   // cached tokens this row sees
+      float m = -INFINITY, l = 0.f;
+      bool ok = true;
+      for (int j = 0; j < steps; ++j) {
+        const int kv0 = x.kv_begin + (x.solo ? 2 * j + t : j) * kChunkKvTile;
+        ok = wait_warp(bar(kBarS + t), n_s & 1, stop);
+        if (!ok) break;
+        ++n_s;
+        fence_after();
+        float s[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld(s + 32 * c, s_tmem + 32 * c);
+        wait_ld();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) settle(s + 32 * c);
+        const int limit = sees - kv0;
+        if (__any_sync(0xffffffffu, limit < kChunkKvTile)) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c) s[c] = c < limit ? s[c] : -INFINITY;
+        }
+        float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int c = 4; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
+        const float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        if (j == 0) {
+          m = tile_max;
+        } else if (__any_sync(0xffffffffu, (tile_max - m) * rs > kMaxSlack)) {
+          // the product of the step before has finished: its completion comes before that of this step's scores
+          const float to = fmaxf(m, tile_max);
+          const float alpha = to == -INFINITY ? 1.f : ex2((m - to) * rs);
+          m = to;
+          l *= alpha;
+#pragma unroll
+          for (int c = 0; c < D; c += 32) {
+            float o[32];
+            tmem_ld(o, o_tmem + c);
+            wait_ld();
+            settle(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] *= alpha;
+            tmem_st(o_tmem + c, reinterpret_cast<const uint32_t*>(o));
+          }
+        }
+        const float shift = m == -INFINITY ? 0.f : m * rs;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            const float a = ex2(fmaf(s[64 * half + 2 * c], rs, -shift)), b = ex2(fmaf(s[64 * half + 2 * c + 1], rs, -shift));
+            sum[(2 * c) & 3] += a;
+            sum[(2 * c + 1) & 3] += b;
+            pk[c] = pack<kBf16>(a, b);
+          }
+          tmem_st(s_tmem + 32 * half, pk);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        wait_st();
+        fence_before();
+        arrive(bar(kBarP + t));
+      }
+      if (!ok) break;
+      // ---- the result
+      if (x.steps > 0) {
+        if (!wait_warp(bar(kBarO + t), n_o & 1, stop)) break;
+        ++n_o;
+        fence_after();
+      }
+      float w = 1.f;     // weight of this group's part
+      if (x.solo && x.steps > 0) {
+        // group 1 hands its part over in the Q tiles (they are free once group 0's products are done too); group 0 merges
+        float* const part = reinterpret_cast<float*>(smem);   // [D][128]
+        if (t == 0) {
+          arrive(bar(kBarMergeFree));
+          if (!wait_warp(bar(kBarMergeFull), n_solo & 1, stop)) break;
+        } else {
+          if (!wait_warp(bar(kBarMergeFree), n_solo & 1, stop)) break;
+          if (steps > 0) {
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+              float o[32];
+              tmem_ld(o, o_tmem + c);
+              wait_ld();
+              settle(o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) part[(c + i) * 128 + row] = o[i];
+            }
+          } else {
+            for (int c = 0; c < D; ++c) part[c * 128 + row] = 0.f;
+          }
+          merge_ml[row] = m;
+          merge_ml[128 + row] = l;
+          arrive(bar(kBarMergeFull));
+          // the tile is the next item's Q once every row of it has been read
+          if (!wait_warp(bar(kBarMergeDone), n_solo & 1, stop)) break;
+        }
+      }
+      if (x.solo && t == 1) {
+        n_solo += x.steps > 0;
+        continue;
+      }
+      float w1 = 0.f;
+      if (x.solo && x.steps > 0) {
+        const float m1 = merge_ml[row], l1 = merge_ml[128 + row];
+        const float to = fmaxf(m, m1);
+        w = to == -INFINITY ? 0.f : ex2((m - to) * rs);
+        w1 = to == -INFINITY ? 0.f : ex2((m1 - to) * rs);
+        l = l * w + l1 * w1;
+        m = to;
+      }
+      const float inv = l > 0.f ? p.v_scale / l : 0.f;
+      const float lse = l > 0.f ? (m * rs + lg2(l)) * 0.6931471805599453f : (l == 0.f ? -INFINITY : l);
+      const int64_t out_row = (int64_t(x.q_start) + token) * p.num_q_heads + q_head;
+      const int64_t part_row = (int64_t(x.slot) + tile_row) * p.num_kv_heads + x.head;
+      if (valid) {
+        if (x.slot >= 0) p.partial_lse[part_row] = lse;
+        else if (p.lse != nullptr) p.lse[out_row] = lse;
+      }
+      const float* const part = reinterpret_cast<const float*>(smem);
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        float o[32];
+        if (x.steps > 0) {
+          tmem_ld(o, o_tmem + c);
+          wait_ld();
+          settle(o);
+          if (x.solo) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = o[i] * w + part[(c + i) * 128 + row] * w1;
+          }
+        }
+        // a row that has seen nothing is zero whatever the accumulator holds
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? o[i] * inv : (l == 0.f ? 0.f : l);
+        if (!valid) continue;
+        if (x.slot >= 0) {
+          float4* dst = reinterpret_cast<float4*>(p.partial_o + part_row * D + c);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        } else {
+          uint4* dst = reinterpret_cast<uint4*>(p.out + out_row * D + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            dst[i] = make_uint4(pack<true>(o[8 * i], o[8 * i + 1]), pack<true>(o[8 * i + 2], o[8 * i + 3]),
+                                pack<true>(o[8 * i + 4], o[8 * i + 5]), pack<true>(o[8 * i + 6], o[8 * i + 7]));
+          }
+        }
+      }
+      if (x.solo && x.steps > 0) {
+        arrive(bar(kBarMergeDone));
+        if (!wait_warp(bar(kBarMergeDone), n_solo & 1, stop)) break;
+        ++n_solo;
+      }
+      fence_before();
+    }
+  } else if (warp >= 8 && warp < 12) {
+    if constexpr (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (run && warp == 8) {
+      // ------------------------------------------------------------------ copies
+      constexpr int kN = kFp8 ? Shape::kRawStages : kStages;
+      constexpr int kFull = kFp8 ? kBarRawFull : kBarFull, kEmpty = kFp8 ? kBarRawEmpty : kBarEmpty;
+      constexpr int kStageBytes = kFp8 ? Shape::kRawBytes : Shape::kTileBytes;
+      constexpr int kBoxes = kFp8 ? 1 : D / 64;                     // per page
+      const uint32_t dst0 = kFp8 ? raw : ring;
+      const int tile_pages_shift = 7 - p.page_shift;                // 128 tokens are 8, 4 or 2 pages
+      const int my_page = lane & ((1 << tile_pages_shift) - 1), my_box = lane >> tile_pages_shift;
+      const int page_tokens = 1 << p.page_shift;
+      int stage = 0;
+      uint32_t phase = 0, n_tail = 0, n_loads = 0;
+      bool ok = true;
+      for (int u = blockIdx.x; ok && u < p.num_units; u += gridDim.x) {
+        const ChunkUnit x = load_unit(p, u);
+        if (x.steps == 0) continue;
+        const int32_t* row = p.block_table + int64_t(x.b) * p.block_table_ld;
+        // this lane's page of step j (every lane of a page holds its id); -1 past the range
+        auto page_of = [&](int j) -> int32_t {
+          const int tok = x.kv_begin + j * kChunkKvTile + (my_page << p.page_shift);
+          if (j >= x.steps || tok >= x.kv_end) return -1;
+          const int32_t id = __ldg(row + (tok >> p.page_shift));
+          if (id < 0 || int64_t(id) >= p.num_pages) {
+            if (my_box == 0) atomicOr(p.error_word, uint32_t(LIBRA_ERR_BAD_PAGE_ID));
+            return int32_t(p.num_pages > 0x7ffffffe ? 0x7ffffffe : p.num_pages);   // past the map's end: reads as zeros
+          }
+          return id;
+        };
+        auto load = [&](const CUtensorMap* map, int j, int32_t page, bool is_v) {
+          const int left = x.kv_end - (x.kv_begin + j * kChunkKvTile);   // live tokens of the tile
+          const int pages = min(kChunkKvTile >> p.page_shift, (left + page_tokens - 1) >> p.page_shift);
+          const bool tail = !kFp8 && is_v && left < kChunkKvTile;
+          if (!wait_warp(bar(kEmpty + stage), phase ^ 1, stop)) return false;
+          const uint32_t signal = tail ? bar(kBarTail) : bar(kFull + stage);
+          const uint32_t dst = dst0 + stage * kStageBytes;
+          if (lane == 0) mbar_expect_tx(signal, uint32_t(pages) * uint32_t(page_tokens) * uint32_t(D * (kFp8 ? 1 : 2)));
+          ++n_loads;
+          __syncwarp();
+          if (my_page < pages && my_box < kBoxes) {
+            int c[3];
+            c[p.pos_head - 1] = x.head;
+            c[p.pos_page - 1] = page;
+            c[p.pos_token - 1] = 0;
+            const uint32_t to = dst + uint32_t(my_box) * (kChunkKvTile * 128) + uint32_t(my_page * page_tokens) * (kFp8 ? D : 128);
+            asm volatile(
+                "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to),
+                "l"(reinterpret_cast<uint64_t>(map)), "r"(signal), "r"(my_box * 64), "r"(c[0]), "r"(c[1]), "r"(c[2])
+                : "memory");
+          }
+          if (tail) {   // rows behind the range are zeroed before the tile is handed on
+            if (!wait_warp(signal, n_tail & 1, stop)) return false;
+            ++n_tail;
+            const int chunks = (kChunkKvTile - left) * (D / 8);
+            for (int i = lane; i < chunks; i += 32) {
+              st_shared(dst + swizzled(left + i / (D / 8), i % (D / 8)), make_uint4(0, 0, 0, 0));
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) arrive(bar(kFull + stage));
+          }
+          if (++stage == kN) {
+            stage = 0;
+            phase ^= 1;
+          }
+          return true;
+        };
+        // in the order in which the products need them: K0, then V and the next K by turns (solo: K one step ahead of V)
+        int32_t cur = page_of(0), next = page_of(1);
+        ok = load(&map_k, 0, cur, false);
+        for (int j = 0; ok && j < x.steps; ++j) {
+          const int32_t after = page_of(j + 2);
+          if (x.solo) {
+            if (j + 1 < x.steps) ok = load(&map_k, j + 1, next, false);
+            if (ok) ok = load(&map_v, j, cur, true);
+          } else {
+            ok = load(&map_v, j, cur, true);
+            if (ok && j + 1 < x.steps) ok = load(&map_k, j + 1, next, false);
+          }
+          cur = next;
+          next = after;
+        }
+      }
+      if (!ok) {   // leave no copy in flight behind: wait (bounded) for the last fill of every stage
+        for (uint32_t s = 0; s < uint32_t(kN) && s < n_loads; ++s) {
+          const uint32_t fill = (n_loads - 1 - s) / kN;
+          for (int i = 0; i < 4096 && !mbar_try_wait(bar(kFull + s), fill & 1); ++i) {}
+        }
+      }
+    } else if (run && warp == 9 && lane == 0) {
+      // ------------------------------------------------------------------ tensor-core instructions
+      constexpr uint32_t kDescS = instr_desc<kBf16>(kChunkKvTile, false), kDescO = instr_desc<kBf16>(D, true);
+      int stage = 0;
+      uint32_t phase = 0, n_q = 0, n_p[2] = {0, 0};
+      bool ok = true;
+      auto next_tile = [&](int& at) {   // the next tile of the ring, once it is there
+        at = stage;
+        if (!wait(bar(kBarFull + stage), phase, stop)) return false;
+        if (++stage == kStages) {
+          stage = 0;
+          phase ^= 1;
+        }
+        fence_after();
+        return true;
+      };
+      auto scores = [&](int t, int q_tile, int k_stage) {   // S_t = Q K^T
+        const uint32_t a0 = q_tiles + q_tile * Shape::kTileBytes, b0 = ring + k_stage * Shape::kTileBytes;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = uint32_t((k >> 2) * (128 * 128) + (k & 3) * 32);
+          mma_ss(tmem + t * 128, smem_desc(a0 + off, 16, 1024), smem_desc(b0 + off, 16, 1024), kDescS, k > 0);
+        }
+        commit(bar(kBarS + t));
+      };
+      auto values = [&](int t, int v_stage, bool first) {   // O_t += P_t V
+        const uint32_t b0 = ring + v_stage * Shape::kTileBytes;
+#pragma unroll
+        for (int k = 0; k < kChunkKvTile / 16; ++k) {
+          mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, smem_desc(b0 + k * 2048, kChunkKvTile * 128, 1024), kDescO,
+                 !(first && k == 0));
+        }
+      };
+      for (int u = blockIdx.x; ok && u < p.num_units; u += gridDim.x) {
+        const ChunkUnit x = load_unit(p, u);
+        ok = wait(bar(kBarQ + 0), n_q & 1, stop) && wait(bar(kBarQ + 1), n_q & 1, stop);
+        ++n_q;
+        if (!ok || x.steps == 0) continue;
+        int k_stage = 0, v_stage = 0;
+        ok = next_tile(k_stage);
+        if (!ok) break;
+        scores(0, 0, k_stage);
+        if (x.solo) {
+          commit(bar(kBarEmpty + k_stage));
+          if (x.steps > 1) {
+            ok = next_tile(k_stage);
+            if (!ok) break;
+            scores(1, 0, k_stage);
+            commit(bar(kBarEmpty + k_stage));
+          }
+          for (int j = 0; ok && j < x.steps; ++j) {
+            const int t = j & 1;
+            ok = next_tile(v_stage) && wait(bar(kBarP + t), n_p[t] & 1, stop);
+            if (!ok) break;
+            ++n_p[t];
+            fence_after();
+            values(t, v_stage, j < 2);
+            commit(bar(kBarEmpty + v_stage));
+            if (j + 2 < x.steps) {
+              ok = next_tile(k_stage);
+              if (!ok) break;
+              scores(t, 0, k_stage);
+              commit(bar(kBarEmpty + k_stage));
+            }
+          }
+          if (ok) {
+            commit(bar(kBarO + 0));
+            commit(bar(kBarO + 1));
+          }
+        } else {
+          scores(1, 1, k_stage);
+          commit(bar(kBarEmpty + k_stage));
+          for (int j = 0; ok && j < x.steps; ++j) {
+            const bool more = j + 1 < x.steps;
+            for (int t = 0; t < 2; ++t) {
+              if (t == 0) ok = next_tile(v_stage);
+              ok = ok && wait(bar(kBarP + t), n_p[t] & 1, stop);
+              if (!ok) break;
+              ++n_p[t];
+              fence_after();
+              values(t, v_stage, j == 0);
+              if (t == 1) commit(bar(kBarEmpty + v_stage));
+              if (!more) {
+                commit(bar(kBarO + t));
+              } else {
+                if (t == 0) ok = next_tile(k_stage);
+                if (!ok) break;
+                scores(t, t, k_stage);
+                if (t == 1) commit(bar(kBarEmpty + k_stage));
+              }
+            }
+          }
+        }
+      }
+      if (!ok) {   // nothing may be in flight when the tensor memory is given back
+        commit(bar(kBarDrain));
+        for (uint32_t i = 0; i < 4096 && !mbar_try_wait(bar(kBarDrain), 0); ++i) {}
+      }
+    }
+  } else if (kFp8 && warp >= 12) {
+    if constexpr (kFp8) {
+      // ------------------------------------------------------------------ E4M3 codes -> fp16 tiles
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+      if (run) {
+        const int tid = threadIdx.x - 384;
+        int stage = 0, rstage = 0;
+        uint32_t phase = 0, rphase = 0;
+        bool ok = true;
+        for (int u = blockIdx.x; ok && u < p.num_units; u += gridDim.x) {
+          const ChunkUnit x = load_unit(p, u);
+          for (int i = 0; ok && i < 2 * x.steps; ++i) {
+            // which step's V this tile is (K tiles need no zeroing): the order of the copies
+            int v_step = -1;
+            if (i > 0) {
+              if (x.solo) v_step = (i & 1) == 0 ? i / 2 - 1 : (i == 2 * x.steps - 1 ? x.steps - 1 : -1);
+              else v_step = (i & 1) ? i / 2 : -1;
+            }
+            const int live = v_step < 0 ? kChunkKvTile : x.kv_end - (x.kv_begin + v_step * kChunkKvTile);
+            ok = wait_warp(bar(kBarRawFull + rstage), rphase, stop) && wait_warp(bar(kBarEmpty + stage), phase ^ 1, stop);
+            if (!ok) break;
+            const uint8_t* src = smem + Shape::kRaw + rstage * Shape::kRawBytes;
+            const uint32_t dst = ring + stage * Shape::kTileBytes;
+            constexpr int kVec = D / 16;   // 16-byte vectors of codes per token
+#pragma unroll 4
+            for (int v = tid; v < kChunkKvTile * kVec; v += 128) {
+              const int r = v / kVec, c = v % kVec;
+              uint4 in = *reinterpret_cast<const uint4*>(src + r * D + c * 16);
+              if (r >= live) in = make_uint4(0, 0, 0, 0);
+              uint4 lo, hi;
+              cvt_e4m3x4(in.x, lo.x, lo.y);
+              cvt_e4m3x4(in.y, lo.z, lo.w);
+              cvt_e4m3x4(in.z, hi.x, hi.y);
+              cvt_e4m3x4(in.w, hi.z, hi.w);
+              // the two 64-channel halves store their even and odd vectors in opposite order: no bank conflicts
+              const bool flip = (c >> 2) & 1;
+              st_shared(dst + swizzled(r, 2 * c + (flip ? 1 : 0)), flip ? hi : lo);
+              st_shared(dst + swizzled(r, 2 * c + (flip ? 0 : 1)), flip ? lo : hi);
+            }
+            fence_proxy_async();
+            arrive(bar(kBarFull + stage));
+            arrive(bar(kBarRawEmpty + rstage));
+            if (++stage == kStages) { stage = 0; phase ^= 1; }
+            if (++rstage == Shape::kRawStages) { rstage = 0; rphase ^= 1; }
+          }
+        }
+      }
+    }
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == 9) tmem_dealloc(tmem, kTmemColumns);
+}
+
+struct ChunkMergeParams {
+  const int4* merges;         // two per ChunkMerge
+  const uint32_t* serial_at;
+  const float* partial_o;
+  const float* partial_lse;
+  __nv_bfloat16* out;
+  float* lse;
+  uint32_t serial;
+  int32_t num_q_heads, num_kv_heads, group;
+};
+
+constexpr int kChunkMergeWarps = 8;
+
+// Log-sum-exp merge of the chunks of a cut item: one warp per row, chunks added in order (no dependence on scheduling).
+// grid = (merges x KV heads, ceil(kChunkItemRows / kChunkMergeWarps))
+template <int D>
+__global__ void __launch_bounds__(kChunkMergeWarps * 32) chunk_merge_kernel(const ChunkMergeParams p) {
+  if (__ldg(p.serial_at) != p.serial) return;   // the attention kernel has said so
+  constexpr int V = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int4 a = __ldg(p.merges + 2 * (blockIdx.x / p.num_kv_heads)), b = __ldg(p.merges + 2 * (blockIdx.x / p.num_kv_heads) + 1);
+  const int head = blockIdx.x % p.num_kv_heads, n_rows = a.z, n = b.x;
+  const int r = blockIdx.y * kChunkMergeWarps + (threadIdx.x >> 5);
+  if (r >= n_rows) return;
+  const int64_t first = (int64_t(a.w) + r) * p.num_kv_heads + head, pitch = int64_t(n_rows) * p.num_kv_heads;
+  const float l0 = lane < n ? p.partial_lse[first + lane * pitch] : -INFINITY;
+  const float l1 = lane + 32 < n ? p.partial_lse[first + (lane + 32) * pitch] : -INFINITY;
+  float m = fmaxf(l0, l1);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  if (m == -INFINITY) m = 0.f;
+  const float w0 = __expf(l0 - m), w1 = __expf(l1 - m);
+  float den = 0.f, num[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) num[v] = 0.f;
+  const float* src = p.partial_o + first * D + lane * V;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const float w = __shfl_sync(0xffffffffu, i < 32 ? w0 : w1, i & 31);
+    den += w;
+#pragma unroll
+    for (int v = 0; v < V; ++v) num[v] += w * src[int64_t(i) * pitch * D + v];
+  }
+  const float inv = den > 0.f ? 1.f / den : 0.f;
+  const int flat = a.y + r, token = flat / p.group;
+  const int64_t row = (int64_t(a.x) + token) * p.num_q_heads + head * p.group + flat - token * p.group;
+  if (p.lse != nullptr && lane == 0) p.lse[row] = den > 0.f ? m + __logf(den) : -INFINITY;
+#pragma unroll
+  for (int v = 0; v < V; v += 2) {
+    *reinterpret_cast<__nv_bfloat162*>(p.out + row * D + lane * V + v) = __floats2bfloat162_rn(num[v] * inv, num[v + 1] * inv);
+  }
+}
+
+}  // namespace libra

@@ -3,6 +3,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <vector>
 
@@ -97,6 +98,23 @@ struct libra_handle_s {
   int next_map = 0;
   int pos_head = 0, pos_page = 0, pos_token = 0;
 
+  // chunk attention: its own plan, workspace and tensor maps
+  struct Chunk {
+    bool planned = false;
+    uint32_t serial = 0;              // of the plan, also in the workspace
+    void* workspace = nullptr;
+    int32_t n_items = 0, n_merges = 0;
+    size_t merges_off = 0, lse_off = 0, o_off = 0;
+    PoolMaps maps[kMapCache];
+    int next_map = 0;
+    int pos_head = 0, pos_page = 0, pos_token = 0;
+    void* staging[2] = {nullptr, nullptr};   // pinned, grown when a plan needs more
+    size_t staging_bytes[2] = {0, 0};
+    cudaEvent_t staging_done[2] = {nullptr, nullptr};
+    int next_staging = 0;
+    bool attributes_set = false;
+  } chunk;
+
   // profiling
   bool profiling = false;
   std::vector<cudaEvent_t> events;  // 3 per call
@@ -110,6 +128,42 @@ inline int fail_cuda(libra_handle_t h, cudaError_t e) {
   if (h) h->last_cuda_error = int(e);
   (void)cudaGetLastError();
   return LIBRA_CUDA_ERROR;
+}
+
+// Tiled tensor map of one pool: dimension 0 is head_dim (contiguous); the other three (token, head, page) are ordered by
+// increasing stride.  Box = row_bytes of a row x box_tokens tokens of one head and page; pos_* receive the coordinate slots.
+inline int encode_pool_map(libra_handle_t h, const void* base, int row_bytes, int box_tokens, CUtensorMapSwizzle swizzle,
+                           CUtensorMap* map, int* pos_head, int* pos_page, int* pos_token) {
+  struct Dim {
+    int64_t stride, size;
+    uint32_t box;
+    int kind;
+  };
+  Dim dims[3] = {{h->stride_token, h->cfg.page_size, uint32_t(box_tokens), 0},
+                 {h->stride_head, h->cfg.num_kv_heads, 1u, 1},
+                 {h->stride_page, h->cfg.num_pages, 1u, 2}};
+  std::stable_sort(dims, dims + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  const int eb = h->fp8 ? 1 : 2;   // bytes per element
+  cuuint64_t gdim[4] = {cuuint64_t(h->cfg.head_dim), 0, 0, 0};
+  cuuint64_t gstride[3];
+  cuuint32_t box[4] = {cuuint32_t(row_bytes / eb), 0, 0, 0};
+  cuuint32_t estride[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 3; ++i) {
+    gdim[i + 1] = cuuint64_t(dims[i].size);
+    gstride[i] = cuuint64_t(dims[i].stride) * eb;
+    box[i + 1] = dims[i].box;
+    if (dims[i].kind == 0) *pos_token = i + 1;
+    if (dims[i].kind == 1) *pos_head = i + 1;
+    if (dims[i].kind == 2) *pos_page = i + 1;
+  }
+  const CUresult r = h->encode(map, h->fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                               const_cast<void*>(base), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    h->last_cuda_error = int(cudaErrorInvalidValue);
+    return LIBRA_CUDA_ERROR;
+  }
+  return LIBRA_OK;
 }
 
 #define LIBRA_CUDA_TRY(h, expr)                       \

@@ -172,42 +172,13 @@ libra::PlanParams resolve_params(const libra_plan_params_t& in, int n_sm_device,
   return p;
 }
 
-// Build the tiled tensor map of one pool: dimension 0 is head_dim (contiguous); the other three
-// (token, head, page) are ordered by increasing stride.  Box = 64 elements x 16 tokens x 1 x 1 (a page of
-// 32 or 64 tokens is read as 2 or 4 such boxes at token offsets 0, 16, ...).
+// Map of one pool for the decode kernel: boxes of 128 bytes (the whole 64-byte row of an 8-bit cache at head_dim 64) x 16
+// tokens; a page of 32 or 64 tokens is read as 2 or 4 such boxes at token offsets 0, 16, ...
 int encode_pool_map(libra_handle_t h, const void* base, CUtensorMap* map, int* pos_head, int* pos_page, int* pos_token) {
-  struct Dim {
-    int64_t stride, size;
-    uint32_t box;
-    int kind;
-  };
-  Dim dims[3] = {{h->stride_token, h->cfg.page_size, 16u, 0},
-                 {h->stride_head, h->cfg.num_kv_heads, 1u, 1},
-                 {h->stride_page, h->cfg.num_pages, 1u, 2}};
-  std::stable_sort(dims, dims + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
-  const int eb = h->fp8 ? 1 : 2;   // bytes per element; a box row is 128 bytes, or the whole 64-byte row of an 8-bit cache at head_dim 64
-  const int row_bytes = std::min(128, h->cfg.head_dim * eb);
-  cuuint64_t gdim[4] = {cuuint64_t(h->cfg.head_dim), 0, 0, 0};
-  cuuint64_t gstride[3];
-  cuuint32_t box[4] = {cuuint32_t(row_bytes / eb), 0, 0, 0};
-  cuuint32_t estride[4] = {1, 1, 1, 1};
-  for (int i = 0; i < 3; ++i) {
-    gdim[i + 1] = cuuint64_t(dims[i].size);
-    gstride[i] = cuuint64_t(dims[i].stride) * eb;
-    box[i + 1] = dims[i].box;
-    if (dims[i].kind == 0) *pos_token = i + 1;
-    if (dims[i].kind == 1) *pos_head = i + 1;
-    if (dims[i].kind == 2) *pos_page = i + 1;
-  }
-  CUresult r = h->encode(map, h->fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), gdim, gstride, box, estride,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) {
-    h->last_cuda_error = int(cudaErrorInvalidValue);
-    return LIBRA_CUDA_ERROR;
-  }
-  return LIBRA_OK;
+  const int row_bytes = std::min(128, h->cfg.head_dim * (h->fp8 ? 1 : 2));
+  return libra::encode_pool_map(h, base, row_bytes, 16,
+                                row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, map, pos_head,
+                                pos_page, pos_token);
 }
 
 // Two slots per SM are the planner's default where a step has two column tiles (kVariantPair, kFp8Pair) and for every
@@ -470,6 +441,8 @@ int libra_destroy(libra_handle_t h) {
     for (int i = 0; i < 2; ++i) {
       if (h->staging_done[i]) cudaEventDestroy(h->staging_done[i]);
       if (h->staging[i]) cudaFreeHost(h->staging[i]);
+      if (h->chunk.staging_done[i]) cudaEventDestroy(h->chunk.staging_done[i]);
+      if (h->chunk.staging[i]) cudaFreeHost(h->chunk.staging[i]);
     }
     for (cudaEvent_t ev : h->events) cudaEventDestroy(ev);
     (void)cudaGetLastError();
@@ -734,7 +707,10 @@ int libra_set_kv_dtype(libra_handle_t h, int32_t dtype, float k_scale, float v_s
   h->fp8_variant = -1;
   h->k_scale = h->fp8 ? k_scale : 1.f;
   h->v_scale = h->fp8 ? v_scale : 1.f;
-  for (int i = 0; i < libra_handle_s::kMapCache; ++i) h->maps[i].k_ptr = h->maps[i].v_ptr = nullptr;  // maps depend on the type
+  for (int i = 0; i < libra_handle_s::kMapCache; ++i) {  // maps depend on the type
+    h->maps[i].k_ptr = h->maps[i].v_ptr = nullptr;
+    h->chunk.maps[i].k_ptr = h->chunk.maps[i].v_ptr = nullptr;
+  }
   return LIBRA_OK;
 }
 
