@@ -22,12 +22,12 @@ typedef void (*ChunkKernelFn)(const CUtensorMap, const CUtensorMap, const libra:
 struct ChunkBuild {
   ChunkKernelFn fn;
   int threads, smem;
-  int registers;   // what the roles hold together after their setmaxnreg: never more than the launch brings
+  int registers;   // that the roles' setmaxnreg counts on
 };
 template <int D, bool kFp8>
 ChunkBuild build_of() {
   using S = libra::ChunkShape<D, kFp8>;
-  return {libra::chunk_kernel<D, kFp8>, S::kThreads, S::kDynamicBytes, kFp8 ? 128 * (2 * 176 + 64 + 96) : 128 * (2 * 232 + 40)};
+  return {libra::chunk_kernel<D, kFp8>, S::kThreads, S::kDynamicBytes, S::kLaunchRegs};
 }
 const ChunkBuild kBuilds[2][2] = {{build_of<64, false>(), build_of<64, true>()}, {build_of<128, false>(), build_of<128, true>()}};
 

@@ -68,6 +68,10 @@ struct ChunkShape {
   static constexpr int kStages = kFp8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);
   static constexpr int kRawStages = kFp8 ? (D == 128 ? 4 : 8) : 0;
   static constexpr int kThreads = kFp8 ? 512 : 384;
+  // registers a thread of each role: together what the launch brings (384 x 168, 512 x 128)
+  static constexpr int kSoftmaxRegs = kFp8 ? 168 : 216, kIssueRegs = kFp8 ? 80 : 72, kConvertRegs = 96;
+  static constexpr int kLaunchRegs = kFp8 ? 512 * 128 : 384 * 168;
+  static_assert(256 * kSoftmaxRegs + 128 * kIssueRegs + (kFp8 ? 128 * kConvertRegs : 0) <= kLaunchRegs, "setmaxnreg would wait");
   // dynamic shared memory: Q tiles | ring | raw ring | floats | barriers
   static constexpr int kRing = 2 * kTileBytes;
   static constexpr int kRaw = kRing + kStages * kTileBytes;
@@ -121,40 +125,47 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// 32 columns of this warp's 32 lanes: register i of a thread is column i of its lane
-__device__ __forceinline__ void tmem_ld(float* r, uint32_t addr) {
+// 16 or 32 columns of this warp's 32 lanes: register i of a thread is column i of its lane
+__device__ __forceinline__ void tmem_ld16(float* r, uint32_t addr) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+        "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ld32(float* r, uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
       : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
         "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]),
         "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]),
         "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
       : "r"(addr));
 }
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 // Uses of these registers come after the wait that precedes this in the program.
+template <int N>
 __device__ __forceinline__ void settle(float* r) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(r[i]));
-}
-__device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(
-          addr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
-      "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
-      "r"(r[31])
-      : "memory");
+  for (int i = 0; i < N; ++i) asm volatile("" : "+f"(r[i]));
 }
 
 // Shared-memory matrix descriptor, 128-byte swizzle.  K-major tiles (Q, K: channels contiguous): `sbo` is the distance of
 // 8-row groups and `lbo` is not read.  MN-major tiles (V: the channels are the N of the product): `lbo` is the distance of
 // 64-channel groups, `sbo` that of 8-token groups.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  return uint64_t((addr >> 4) & 0x3fff) | (uint64_t(lbo >> 4) << 16) | (uint64_t(sbo >> 4) << 32) | (uint64_t(1) << 46) |
-         (uint64_t(2) << 61);
+// The address field counts 16 bytes, so that a step within a tile is an addition to the lower word.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);   // sbo 1024, descriptor version, 128-byte swizzle
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lbo) { return (addr >> 4) | ((lbo >> 4) << 16); }
+__device__ __forceinline__ uint64_t smem_desc(uint32_t low) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(kDescHigh));
+  return d;
 }
 // Instruction descriptor: fp32 accumulation, 16-bit operands (bf16 or fp16), M = 128
 template <bool kBf16>
@@ -226,6 +237,10 @@ struct ChunkUnit {
   int head;    // KV head
   int steps;   // of 128 cached tokens
   bool solo;   // one row tile, the softmax groups take turns on the steps
+  // Tile i of the ring, in the order in which the products need them: K of step 0, then V of a step and K of the next by turns;
+  // solo: K runs one step further ahead.
+  __device__ __forceinline__ bool is_v(int i) const { return solo ? i > 0 && ((i & 1) == 0 || i == 2 * steps - 1) : (i & 1); }
+  __device__ __forceinline__ int step_of(int i) const { return solo ? (is_v(i) ? (i == 2 * steps - 1 ? steps - 1 : (i >> 1) - 1) : (i + 1) >> 1) : i >> 1; }
   // steps of row tile (softmax group) t
   __device__ __forceinline__ int steps_of(int t) const { return solo ? (steps + 1 - t) >> 1 : steps; }
 };
@@ -297,8 +312,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 
   if (run && warp < 8) {
     // ------------------------------------------------------------------ softmax group t: row tile t (both: tile 0 if solo)
-    if constexpr (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kSoftmaxRegs));
     const int t = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const uint32_t s_tmem = tmem + lanes + t * 128, o_tmem = tmem + lanes + 256 + t * 128;
@@ -362,10 +376,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         fence_after();
         float s[128];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld(s + 32 * c, s_tmem + 32 * c);
+        for (int c = 0; c < 4; ++c) tmem_ld32(s + 32 * c, s_tmem + 32 * c);
         wait_ld();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) settle(s + 32 * c);
+        for (int c = 0; c < 4; ++c) settle<32>(s + 32 * c);
         const int limit = sees - kv0;
         if (__any_sync(0xffffffffu, limit < kChunkKvTile)) {
 #pragma unroll
@@ -384,29 +398,30 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           m = to;
           l *= alpha;
 #pragma unroll
-          for (int c = 0; c < D; c += 32) {
-            float o[32];
-            tmem_ld(o, o_tmem + c);
+          for (int c = 0; c < D; c += 16) {
+            float o[16];
+            tmem_ld16(o, o_tmem + c);
             wait_ld();
-            settle(o);
+            settle<16>(o);
+            uint32_t scaled[16];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] *= alpha;
-            tmem_st(o_tmem + c, reinterpret_cast<const uint32_t*>(o));
+            for (int i = 0; i < 16; ++i) scaled[i] = __float_as_uint(o[i] * alpha);
+            tmem_st16(o_tmem + c, scaled);
           }
         }
         const float shift = m == -INFINITY ? 0.f : m * rs;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t pk[32];
+        for (int part = 0; part < 4; ++part) {
+          uint32_t pk[16];
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            const float a = ex2(fmaf(s[64 * half + 2 * c], rs, -shift)), b = ex2(fmaf(s[64 * half + 2 * c + 1], rs, -shift));
+          for (int c = 0; c < 16; ++c) {
+            const float a = ex2(fmaf(s[32 * part + 2 * c], rs, -shift)), b = ex2(fmaf(s[32 * part + 2 * c + 1], rs, -shift));
             sum[(2 * c) & 3] += a;
             sum[(2 * c + 1) & 3] += b;
             pk[c] = pack<kBf16>(a, b);
           }
-          tmem_st(s_tmem + 32 * half, pk);
+          tmem_st16(s_tmem + 16 * part, pk);
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         wait_st();
@@ -433,9 +448,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
               float o[32];
-              tmem_ld(o, o_tmem + c);
+              tmem_ld32(o, o_tmem + c);
               wait_ld();
-              settle(o);
+              settle<32>(o);
 #pragma unroll
               for (int i = 0; i < 32; ++i) part[(c + i) * 128 + row] = o[i];
             }
@@ -475,9 +490,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       for (int c = 0; c < D; c += 32) {
         float o[32];
         if (x.steps > 0) {
-          tmem_ld(o, o_tmem + c);
+          tmem_ld32(o, o_tmem + c);
           wait_ld();
-          settle(o);
+          settle<32>(o);
           if (x.solo) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] = o[i] * w + part[(c + i) * 128 + row] * w1;
@@ -508,8 +523,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       fence_before();
     }
   } else if (warp >= 8 && warp < 12) {
-    if constexpr (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kIssueRegs));
     if (run && warp == 8) {
       // ------------------------------------------------------------------ copies
       constexpr int kN = kFp8 ? Shape::kRawStages : kStages;
@@ -538,33 +552,38 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
           return id;
         };
-        auto load = [&](const CUtensorMap* map, int j, int32_t page, bool is_v) {
-          const int left = x.kv_end - (x.kv_begin + j * kChunkKvTile);   // live tokens of the tile
+        int32_t next = page_of(0);
+        for (int i = 0; i < 2 * x.steps; ++i) {
+          const bool is_v = x.is_v(i);
+          const int left = x.kv_end - (x.kv_begin + x.step_of(i) * kChunkKvTile);   // live tokens from the tile's first on
+          const int32_t page = next;
+          next = page_of(i + 1 < 2 * x.steps ? x.step_of(i + 1) : x.steps);
           const int pages = min(kChunkKvTile >> p.page_shift, (left + page_tokens - 1) >> p.page_shift);
           const bool tail = !kFp8 && is_v && left < kChunkKvTile;
-          if (!wait_warp(bar(kEmpty + stage), phase ^ 1, stop)) return false;
+          ok = wait_warp(bar(kEmpty + stage), phase ^ 1, stop);
+          if (!ok) break;
           const uint32_t signal = tail ? bar(kBarTail) : bar(kFull + stage);
           const uint32_t dst = dst0 + stage * kStageBytes;
           if (lane == 0) mbar_expect_tx(signal, uint32_t(pages) * uint32_t(page_tokens) * uint32_t(D * (kFp8 ? 1 : 2)));
           ++n_loads;
           __syncwarp();
           if (my_page < pages && my_box < kBoxes) {
-            int c[3];
-            c[p.pos_head - 1] = x.head;
-            c[p.pos_page - 1] = page;
-            c[p.pos_token - 1] = 0;
+            const int c1 = p.pos_head == 1 ? x.head : (p.pos_page == 1 ? page : 0);
+            const int c2 = p.pos_head == 2 ? x.head : (p.pos_page == 2 ? page : 0);
+            const int c3 = p.pos_head == 3 ? x.head : (p.pos_page == 3 ? page : 0);
             const uint32_t to = dst + uint32_t(my_box) * (kChunkKvTile * 128) + uint32_t(my_page * page_tokens) * (kFp8 ? D : 128);
             asm volatile(
                 "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to),
-                "l"(reinterpret_cast<uint64_t>(map)), "r"(signal), "r"(my_box * 64), "r"(c[0]), "r"(c[1]), "r"(c[2])
+                "l"(reinterpret_cast<uint64_t>(is_v ? &map_v : &map_k)), "r"(signal), "r"(my_box * 64), "r"(c1), "r"(c2), "r"(c3)
                 : "memory");
           }
           if (tail) {   // rows behind the range are zeroed before the tile is handed on
-            if (!wait_warp(signal, n_tail & 1, stop)) return false;
+            ok = wait_warp(signal, n_tail & 1, stop);
+            if (!ok) break;
             ++n_tail;
             const int chunks = (kChunkKvTile - left) * (D / 8);
-            for (int i = lane; i < chunks; i += 32) {
-              st_shared(dst + swizzled(left + i / (D / 8), i % (D / 8)), make_uint4(0, 0, 0, 0));
+            for (int k = lane; k < chunks; k += 32) {
+              st_shared(dst + swizzled(left + k / (D / 8), k % (D / 8)), make_uint4(0, 0, 0, 0));
             }
             fence_proxy_async();
             __syncwarp();
@@ -574,22 +593,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             stage = 0;
             phase ^= 1;
           }
-          return true;
-        };
-        // in the order in which the products need them: K0, then V and the next K by turns (solo: K one step ahead of V)
-        int32_t cur = page_of(0), next = page_of(1);
-        ok = load(&map_k, 0, cur, false);
-        for (int j = 0; ok && j < x.steps; ++j) {
-          const int32_t after = page_of(j + 2);
-          if (x.solo) {
-            if (j + 1 < x.steps) ok = load(&map_k, j + 1, next, false);
-            if (ok) ok = load(&map_v, j, cur, true);
-          } else {
-            ok = load(&map_v, j, cur, true);
-            if (ok && j + 1 < x.steps) ok = load(&map_k, j + 1, next, false);
-          }
-          cur = next;
-          next = after;
         }
       }
       if (!ok) {   // leave no copy in flight behind: wait (bounded) for the last fill of every stage
@@ -615,19 +618,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         return true;
       };
       auto scores = [&](int t, int q_tile, int k_stage) {   // S_t = Q K^T
-        const uint32_t a0 = q_tiles + q_tile * Shape::kTileBytes, b0 = ring + k_stage * Shape::kTileBytes;
+        const uint32_t a0 = desc_low(q_tiles + q_tile * Shape::kTileBytes, 0), b0 = desc_low(ring + k_stage * Shape::kTileBytes, 0);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = uint32_t((k >> 2) * (128 * 128) + (k & 3) * 32);
-          mma_ss(tmem + t * 128, smem_desc(a0 + off, 16, 1024), smem_desc(b0 + off, 16, 1024), kDescS, k > 0);
+          const uint32_t off = uint32_t((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+          mma_ss(tmem + t * 128, smem_desc(a0 + off), smem_desc(b0 + off), kDescS, k > 0);
         }
         commit(bar(kBarS + t));
       };
       auto values = [&](int t, int v_stage, bool first) {   // O_t += P_t V
-        const uint32_t b0 = ring + v_stage * Shape::kTileBytes;
+        const uint32_t b0 = desc_low(ring + v_stage * Shape::kTileBytes, kChunkKvTile * 128);
 #pragma unroll
         for (int k = 0; k < kChunkKvTile / 16; ++k) {
-          mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, smem_desc(b0 + k * 2048, kChunkKvTile * 128, 1024), kDescO,
+          mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, smem_desc(b0 + k * (2048 >> 4)), kDescO,
                  !(first && k == 0));
         }
       };
@@ -636,61 +639,30 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         ok = wait(bar(kBarQ + 0), n_q & 1, stop) && wait(bar(kBarQ + 1), n_q & 1, stop);
         ++n_q;
         if (!ok || x.steps == 0) continue;
+        // turn i: pair: row tile i & 1 at step i / 2, the two share the tiles of K and V; solo: step i, row tile 0, group i & 1
+        const int turns = x.solo ? x.steps : 2 * x.steps;
         int k_stage = 0, v_stage = 0;
-        ok = next_tile(k_stage);
-        if (!ok) break;
-        scores(0, 0, k_stage);
-        if (x.solo) {
-          commit(bar(kBarEmpty + k_stage));
-          if (x.steps > 1) {
-            ok = next_tile(k_stage);
-            if (!ok) break;
-            scores(1, 0, k_stage);
-            commit(bar(kBarEmpty + k_stage));
-          }
-          for (int j = 0; ok && j < x.steps; ++j) {
-            const int t = j & 1;
-            ok = next_tile(v_stage) && wait(bar(kBarP + t), n_p[t] & 1, stop);
+        for (int i = -2; i < turns; ++i) {
+          const int t = i & 1;
+          const bool first = x.solo || t == 0, last = x.solo || t == 1;   // of the turns that use a tile
+          if (i >= 0) {
+            if (first) ok = next_tile(v_stage);
+            ok = ok && wait(bar(kBarP + t), n_p[t] & 1, stop);
             if (!ok) break;
             ++n_p[t];
             fence_after();
-            values(t, v_stage, j < 2);
-            commit(bar(kBarEmpty + v_stage));
-            if (j + 2 < x.steps) {
-              ok = next_tile(k_stage);
-              if (!ok) break;
-              scores(t, 0, k_stage);
-              commit(bar(kBarEmpty + k_stage));
-            }
+            values(t, v_stage, i < 2);
+            if (last) commit(bar(kBarEmpty + v_stage));
+            if (i + 2 >= turns) commit(bar(kBarO + t));
           }
-          if (ok) {
-            commit(bar(kBarO + 0));
-            commit(bar(kBarO + 1));
-          }
-        } else {
-          scores(1, 1, k_stage);
-          commit(bar(kBarEmpty + k_stage));
-          for (int j = 0; ok && j < x.steps; ++j) {
-            const bool more = j + 1 < x.steps;
-            for (int t = 0; t < 2; ++t) {
-              if (t == 0) ok = next_tile(v_stage);
-              ok = ok && wait(bar(kBarP + t), n_p[t] & 1, stop);
-              if (!ok) break;
-              ++n_p[t];
-              fence_after();
-              values(t, v_stage, j == 0);
-              if (t == 1) commit(bar(kBarEmpty + v_stage));
-              if (!more) {
-                commit(bar(kBarO + t));
-              } else {
-                if (t == 0) ok = next_tile(k_stage);
-                if (!ok) break;
-                scores(t, t, k_stage);
-                if (t == 1) commit(bar(kBarEmpty + k_stage));
-              }
-            }
+          if (i + 2 < turns) {
+            if (first) ok = next_tile(k_stage);
+            if (!ok) break;
+            scores(t, x.solo ? 0 : t, k_stage);
+            if (last) commit(bar(kBarEmpty + k_stage));
           }
         }
+        if (ok && turns == 1) commit(bar(kBarO + 1));   // group 1 has no turn
       }
       if (!ok) {   // nothing may be in flight when the tensor memory is given back
         commit(bar(kBarDrain));
@@ -700,7 +672,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   } else if (kFp8 && warp >= 12) {
     if constexpr (kFp8) {
       // ------------------------------------------------------------------ E4M3 codes -> fp16 tiles
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kConvertRegs));
       if (run) {
         const int tid = threadIdx.x - 384;
         int stage = 0, rstage = 0;
@@ -709,13 +681,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         for (int u = blockIdx.x; ok && u < p.num_units; u += gridDim.x) {
           const ChunkUnit x = load_unit(p, u);
           for (int i = 0; ok && i < 2 * x.steps; ++i) {
-            // which step's V this tile is (K tiles need no zeroing): the order of the copies
-            int v_step = -1;
-            if (i > 0) {
-              if (x.solo) v_step = (i & 1) == 0 ? i / 2 - 1 : (i == 2 * x.steps - 1 ? x.steps - 1 : -1);
-              else v_step = (i & 1) ? i / 2 : -1;
-            }
-            const int live = v_step < 0 ? kChunkKvTile : x.kv_end - (x.kv_begin + v_step * kChunkKvTile);
+            const int live = x.is_v(i) ? x.kv_end - (x.kv_begin + x.step_of(i) * kChunkKvTile) : kChunkKvTile;   // K needs no zeroing
             ok = wait_warp(bar(kBarRawFull + rstage), rphase, stop) && wait_warp(bar(kBarEmpty + stage), phase ^ 1, stop);
             if (!ok) break;
             const uint8_t* src = smem + Shape::kRaw + rstage * Shape::kRawBytes;
