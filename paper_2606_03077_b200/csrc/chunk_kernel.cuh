@@ -87,8 +87,9 @@ using namespace dev;
 
 // barriers, in 8-byte slots after the floats
 constexpr int kBarFull = 0, kBarEmpty = 8, kBarRawFull = 16, kBarRawEmpty = 24, kBarQ = 32, kBarS = 34, kBarP = 36, kBarO = 38,
-              kBarMergeFree = 40, kBarMergeFull = 41, kBarMergeDone = 42, kBarTail = 43, kBarDrain = 44;
-constexpr int kSlotStop = 46, kSlotTmem = 47;   // the stop flag and the tensor-memory address live in two more slots
+              kBarMergeFree = 40, kBarMergeFull = 41, kBarMergeDone = 42, kBarDrain = 43, kBarTail = 44;
+constexpr int kLoaders = 3;   // warps 8, 10 and 11 take the ring's tiles by turns
+constexpr int kSlotStop = 48, kSlotTmem = 49;   // the stop flag and the tensor-memory address live in two more slots
 
 struct Stop {   // how a wait that ran out ends the block
   volatile uint32_t* flag;
@@ -294,7 +295,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     mbar_init(bar(kBarMergeFree), 128);
     mbar_init(bar(kBarMergeFull), 128);
     mbar_init(bar(kBarMergeDone), 128);
-    mbar_init(bar(kBarTail), 1);
+    for (int i = 0; i < kLoaders; ++i) mbar_init(bar(kBarTail + i), 1);
     mbar_init(bar(kBarDrain), 1);
     fence_mbar_init();
     // another plan in the workspace than the one this launch was made for: nothing is computed
@@ -524,8 +525,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     }
   } else if (warp >= 8 && warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kIssueRegs));
-    if (run && warp == 8) {
+    if (run && warp != 9) {
       // ------------------------------------------------------------------ copies
+      const int loader = warp == 8 ? 0 : warp - 9;
       constexpr int kN = kFp8 ? Shape::kRawStages : kStages;
       constexpr int kFull = kFp8 ? kBarRawFull : kBarFull, kEmpty = kFp8 ? kBarRawEmpty : kBarEmpty;
       constexpr int kStageBytes = kFp8 ? Shape::kRawBytes : Shape::kTileBytes;
@@ -534,12 +536,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       const int tile_pages_shift = 7 - p.page_shift;                // 128 tokens are 8, 4 or 2 pages
       const int my_page = lane & ((1 << tile_pages_shift) - 1), my_box = lane >> tile_pages_shift;
       const int page_tokens = 1 << p.page_shift;
-      int stage = 0;
-      uint32_t phase = 0, n_tail = 0, n_loads = 0;
+      uint32_t n_tail = 0;
+      int first = 0, mine = loader;   // tiles of the ring before this item; the next tile that this warp brings
+      int stage = loader % kN;        // of tile `mine`
+      uint32_t phase = loader / kN;
       bool ok = true;
       for (int u = blockIdx.x; ok && u < p.num_units; u += gridDim.x) {
         const ChunkUnit x = load_unit(p, u);
-        if (x.steps == 0) continue;
+        const int end = first + 2 * x.steps;
+        if (mine >= end) {
+          first = end;
+          continue;
+        }
         const int32_t* row = p.block_table + int64_t(x.b) * p.block_table_ld;
         // this lane's page of step j (every lane of a page holds its id); -1 past the range
         auto page_of = [&](int j) -> int32_t {
@@ -552,20 +560,20 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
           return id;
         };
-        int32_t next = page_of(0);
-        for (int i = 0; i < 2 * x.steps; ++i) {
+        int32_t next = page_of(x.step_of(mine - first));
+        for (; mine < end; mine += kLoaders) {
+          const int i = mine - first;
           const bool is_v = x.is_v(i);
           const int left = x.kv_end - (x.kv_begin + x.step_of(i) * kChunkKvTile);   // live tokens from the tile's first on
           const int32_t page = next;
-          next = page_of(i + 1 < 2 * x.steps ? x.step_of(i + 1) : x.steps);
+          next = page_of(mine + kLoaders < end ? x.step_of(i + kLoaders) : x.steps);
           const int pages = min(kChunkKvTile >> p.page_shift, (left + page_tokens - 1) >> p.page_shift);
           const bool tail = !kFp8 && is_v && left < kChunkKvTile;
           ok = wait_warp(bar(kEmpty + stage), phase ^ 1, stop);
           if (!ok) break;
-          const uint32_t signal = tail ? bar(kBarTail) : bar(kFull + stage);
+          const uint32_t signal = tail ? bar(kBarTail + loader) : bar(kFull + stage);
           const uint32_t dst = dst0 + stage * kStageBytes;
           if (lane == 0) mbar_expect_tx(signal, uint32_t(pages) * uint32_t(page_tokens) * uint32_t(D * (kFp8 ? 1 : 2)));
-          ++n_loads;
           __syncwarp();
           if (my_page < pages && my_box < kBoxes) {
             const int c1 = p.pos_head == 1 ? x.head : (p.pos_page == 1 ? page : 0);
@@ -589,16 +597,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             __syncwarp();
             if (lane == 0) arrive(bar(kFull + stage));
           }
-          if (++stage == kN) {
-            stage = 0;
+          stage += kLoaders;
+          if (stage >= kN) {
+            stage -= kN;
             phase ^= 1;
           }
         }
+        first = end;
       }
-      if (!ok) {   // leave no copy in flight behind: wait (bounded) for the last fill of every stage
-        for (uint32_t s = 0; s < uint32_t(kN) && s < n_loads; ++s) {
-          const uint32_t fill = (n_loads - 1 - s) / kN;
-          for (int i = 0; i < 4096 && !mbar_try_wait(bar(kFull + s), fill & 1); ++i) {}
+      if (!ok) {   // leave no copy in flight behind: wait (bounded) for this warp's last fills
+        for (int g = mine - kLoaders; g >= 0 && g >= mine - kN; g -= kLoaders) {
+          for (int i = 0; i < 4096 && !mbar_try_wait(bar(kFull + g % kN), (g / kN) & 1); ++i) {}
         }
       }
     } else if (run && warp == 9 && lane == 0) {
