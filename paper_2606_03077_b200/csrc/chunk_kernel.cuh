@@ -69,7 +69,7 @@ struct ChunkShape {
   static constexpr int kRawStages = kFp8 ? (D == 128 ? 4 : 8) : 0;
   static constexpr int kThreads = kFp8 ? 512 : 384;
   // registers a thread of each role: together what the launch brings (384 x 168, 512 x 128)
-  static constexpr int kSoftmaxRegs = kFp8 ? 168 : 216, kIssueRegs = kFp8 ? 80 : 72, kConvertRegs = 96;
+  static constexpr int kSoftmaxRegs = kFp8 ? 184 : 216, kIssueRegs = 72, kConvertRegs = 72;
   static constexpr int kLaunchRegs = kFp8 ? 512 * 128 : 384 * 168;
   static_assert(256 * kSoftmaxRegs + 128 * kIssueRegs + (kFp8 ? 128 * kConvertRegs : 0) <= kLaunchRegs, "setmaxnreg would wait");
   // dynamic shared memory: Q tiles | ring | raw ring | floats | barriers
@@ -245,8 +245,13 @@ struct ChunkUnit {
   // steps of row tile (softmax group) t
   __device__ __forceinline__ int steps_of(int t) const { return solo ? (steps + 1 - t) >> 1 : steps; }
 };
+__device__ __forceinline__ int4 load_again(const int4* at) {   // not merged with another load of the same address
+  int4 v;
+  asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at));
+  return v;
+}
 __device__ __forceinline__ ChunkUnit load_unit(const ChunkParams& p, int u) {
-  const int4 a = __ldg(p.items + 2 * (u / p.num_kv_heads)), c = __ldg(p.items + 2 * (u / p.num_kv_heads) + 1);
+  const int4 a = load_again(p.items + 2 * (u / p.num_kv_heads)), c = load_again(p.items + 2 * (u / p.num_kv_heads) + 1);
   ChunkUnit x;
   x.b = a.x; x.q_start = a.y; x.row0 = a.z; x.n_rows = a.w;
   x.kv_begin = c.x; x.kv_end = c.y; x.ctx = c.z; x.slot = c.w;
@@ -300,7 +305,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     fence_mbar_init();
     // another plan in the workspace than the one this launch was made for: nothing is computed
     const uint32_t found = *reinterpret_cast<const volatile uint32_t*>(p.serial_at);
-    slots[2 * kSlotStop] = (found != p.serial || (base & 1023u) != 0) ? 1u : 0u;
+    slots[2 * kSlotStop] = found != p.serial ? 1u : 0u;
     if (found != p.serial) atomicOr(p.error_word, uint32_t(LIBRA_ERR_PLAN_CHANGED));
   }
   if (warp == 9) tmem_alloc(bar(kSlotTmem), kTmemColumns);
@@ -319,38 +324,46 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     const uint32_t s_tmem = tmem + lanes + t * 128, o_tmem = tmem + lanes + 256 + t * 128;
     uint32_t n_s = 0, n_q = 0, n_o = 0, n_solo = 0;   // phases seen
     for (int u = blockIdx.x; u < p.num_units; u += gridDim.x) {
-      const ChunkUnit x = load_unit(p, u);
-      const int steps = x.steps_of(t);
-      const int tile_row = (x.solo ? 0 : t * kChunkTileRows) + row;   // row within the item
-      const bool valid = tile_row < x.n_rows;
-      const int token = (x.row0 + (valid ? tile_row : 0)) / p.group;
-      const int q_head = x.head * p.group + (x.row0 + (valid ? tile_row : 0)) - token * p.group;
-      // ---- Q: 16 lanes (8 at D = 64) bring one row
-      if (x.steps > 0 && !(x.solo && t == 1)) {
-        constexpr int kLanes = D / 8, kRowsAtOnce = 128 / kLanes, kBatch = 8;
-        const int c16 = row % kLanes;
+      // what the steps need is kept, the rest of the item is read again where it is used: registers are short here
+      int steps, all_steps, sees, kv0, kv_pitch;
+      bool solo;
+      {
+        const ChunkUnit x = load_unit(p, u);
+        all_steps = x.steps;
+        steps = x.steps_of(t);
+        solo = x.solo;
+        const int tile_row = (solo ? 0 : t * kChunkTileRows) + row;   // row within the item
+        // cached tokens this row sees
+        sees = tile_row < x.n_rows ? min(x.kv_end, x.ctx + (x.row0 + tile_row) / p.group + 1) : 0;
+        kv0 = x.kv_begin + (solo ? t * kChunkKvTile : 0);
+        kv_pitch = solo ? 2 * kChunkKvTile : kChunkKvTile;
+        // ---- Q: 16 lanes (8 at D = 64) bring one row
+        if (x.steps > 0 && !(x.solo && t == 1)) {
+          constexpr int kLanes = D / 8, kRowsAtOnce = 128 / kLanes, kBatch = 8;
+          const int c16 = row % kLanes;
 #pragma unroll 1
-        for (int r0 = row / kLanes; r0 < kChunkTileRows; r0 += kRowsAtOnce * kBatch) {
-          uint4 v[kBatch];
+          for (int r0 = row / kLanes; r0 < kChunkTileRows; r0 += kRowsAtOnce * kBatch) {
+            uint4 v[kBatch];
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int ir = t * kChunkTileRows + r0 + i * kRowsAtOnce;
-            v[i] = make_uint4(0, 0, 0, 0);
-            if (ir < x.n_rows) {
-              const int flat = x.row0 + ir, tok = flat / p.group;
-              v[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (int64_t(x.q_start) + tok) * p.q_stride +
-                                                          int64_t(x.head * p.group + flat - tok * p.group) * D) + c16);
+            for (int i = 0; i < kBatch; ++i) {
+              const int ir = t * kChunkTileRows + r0 + i * kRowsAtOnce;
+              v[i] = make_uint4(0, 0, 0, 0);
+              if (ir < x.n_rows) {
+                const int flat = x.row0 + ir, tok = flat / p.group;
+                v[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (int64_t(x.q_start) + tok) * p.q_stride +
+                                                            int64_t(x.head * p.group + flat - tok * p.group) * D) + c16);
+              }
             }
-          }
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int r = r0 + i * kRowsAtOnce;
-            if constexpr (kFp8) {
-              float down;
-              v[i] = scaled_half_row<kLanes>(v[i], down);
-              if (c16 == 0) row_factor[t * 128 + r] = down;
+            for (int i = 0; i < kBatch; ++i) {
+              const int r = r0 + i * kRowsAtOnce;
+              if constexpr (kFp8) {
+                float down;
+                v[i] = scaled_half_row<kLanes>(v[i], down);
+                if (c16 == 0) row_factor[t * 128 + r] = down;
+              }
+              st_shared(q_tiles + t * Shape::kTileBytes + swizzled(r, c16), v[i]);
             }
-            st_shared(q_tiles + t * Shape::kTileBytes + swizzled(r, c16), v[i]);
           }
         }
       }
@@ -358,19 +371,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       arrive(bar(kBarQ + t));
       if constexpr (kFp8) {
         // the row factors come from the group that loaded the tile
-        if (!wait_warp(bar(kBarQ + (x.solo ? 0 : t)), n_q & 1, stop)) break;
+        if (!wait_warp(bar(kBarQ + (solo ? 0 : t)), n_q & 1, stop)) break;
       }
       ++n_q;
       float rs = p.scale_log2;   // score -> base-2 exponent
       if constexpr (kFp8) {
-        if (x.steps > 0) rs *= row_factor[(x.solo ? 0 : t) * 128 + row];
+        if (all_steps > 0) rs *= row_factor[(solo ? 0 : t) * 128 + row];
       }
       // ---- the steps
-      const int sees = valid ? min(x.kv_end, x.ctx + token + 1) : 0;   // cached tokens this row sees
       float m = -INFINITY, l = 0.f;
       bool ok = true;
-      for (int j = 0; j < steps; ++j) {
-        const int kv0 = x.kv_begin + (x.solo ? 2 * j + t : j) * kChunkKvTile;
+#pragma unroll 1
+      for (int j = 0; j < steps; ++j, kv0 += kv_pitch) {
         ok = wait_warp(bar(kBarS + t), n_s & 1, stop);
         if (!ok) break;
         ++n_s;
@@ -431,13 +443,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       if (!ok) break;
       // ---- the result
-      if (x.steps > 0) {
+      if (all_steps > 0) {
         if (!wait_warp(bar(kBarO + t), n_o & 1, stop)) break;
         ++n_o;
         fence_after();
       }
       float w = 1.f;     // weight of this group's part
-      if (x.solo && x.steps > 0) {
+      if (solo && all_steps > 0) {
         // group 1 hands its part over in the Q tiles (they are free once group 0's products are done too); group 0 merges
         float* const part = reinterpret_cast<float*>(smem);   // [D][128]
         if (t == 0) {
@@ -465,12 +477,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           if (!wait_warp(bar(kBarMergeDone), n_solo & 1, stop)) break;
         }
       }
-      if (x.solo && t == 1) {
-        n_solo += x.steps > 0;
+      if (solo && t == 1) {
+        n_solo += all_steps > 0;
         continue;
       }
       float w1 = 0.f;
-      if (x.solo && x.steps > 0) {
+      if (solo && all_steps > 0) {
         const float m1 = merge_ml[row], l1 = merge_ml[128 + row];
         const float to = fmaxf(m, m1);
         w = to == -INFINITY ? 0.f : ex2((m - to) * rs);
@@ -480,6 +492,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       const float inv = l > 0.f ? p.v_scale / l : 0.f;
       const float lse = l > 0.f ? (m * rs + lg2(l)) * 0.6931471805599453f : (l == 0.f ? -INFINITY : l);
+      const ChunkUnit x = load_unit(p, u);
+      const int tile_row = (solo ? 0 : t * kChunkTileRows) + row;
+      const bool valid = tile_row < x.n_rows;
+      const int token = (x.row0 + (valid ? tile_row : 0)) / p.group;
+      const int q_head = x.head * p.group + (x.row0 + (valid ? tile_row : 0)) - token * p.group;
       const int64_t out_row = (int64_t(x.q_start) + token) * p.num_q_heads + q_head;
       const int64_t part_row = (int64_t(x.slot) + tile_row) * p.num_kv_heads + x.head;
       if (valid) {
@@ -490,11 +507,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
         float o[32];
-        if (x.steps > 0) {
+        if (all_steps > 0) {
           tmem_ld32(o, o_tmem + c);
           wait_ld();
           settle<32>(o);
-          if (x.solo) {
+          if (solo) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] = o[i] * w + part[(c + i) * 128 + row] * w1;
           }
@@ -516,7 +533,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
         }
       }
-      if (x.solo && x.steps > 0) {
+      if (solo && all_steps > 0) {
         arrive(bar(kBarMergeDone));
         if (!wait_warp(bar(kBarMergeDone), n_solo & 1, stop)) break;
         ++n_solo;
