@@ -86,8 +86,9 @@ namespace chunk {
 using namespace dev;
 
 // barriers, in 8-byte slots after the floats
-constexpr int kBarFull = 0, kBarEmpty = 8, kBarRawFull = 16, kBarRawEmpty = 24, kBarQ = 32, kBarS = 34, kBarP = 36, kBarO = 38,
+constexpr int kBarFull = 0, kBarEmpty = 8, kBarRawFull = 16, kBarRawEmpty = 24, kBarQ = 32, kBarS = 34, kBarP = 36, kBarO = 38, kBarPTail = 50,
               kBarMergeFree = 40, kBarMergeFull = 41, kBarMergeDone = 42, kBarDrain = 43, kBarTail = 44;
+constexpr int kPEarly = 3;    // quarters of a step's probabilities that the second product starts on
 constexpr int kLoaders = 3;   // warps 8, 10 and 11 take the ring's tiles by turns
 constexpr int kSlotStop = 48, kSlotTmem = 49;   // the stop flag and the tensor-memory address live in two more slots
 
@@ -189,6 +190,25 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 // Completes on `bar` once everything this thread has issued to the tensor cores is done.
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// Two floats at once, and the largest of three.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<const uint64_t*>(&a)), "l"(*reinterpret_cast<const uint64_t*>(&b)), "l"(*reinterpret_cast<const uint64_t*>(&c)));
+  return *reinterpret_cast<const float2*>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<const uint64_t*>(&a)), "l"(*reinterpret_cast<const uint64_t*>(&b)));
+  return *reinterpret_cast<const float2*>(&d);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.ftz.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 template <bool kBf16>
@@ -295,6 +315,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       mbar_init(bar(kBarQ + t), 128);
       mbar_init(bar(kBarS + t), 1);
       mbar_init(bar(kBarP + t), 128);
+      mbar_init(bar(kBarPTail + t), 128);
       mbar_init(bar(kBarO + t), 1);
     }
     mbar_init(bar(kBarMergeFree), 128);
@@ -400,8 +421,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         }
         float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int c = 4; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
-        const float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        for (int c = 4; c < 124; c += 8) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], s[c + 2 * i], s[c + 2 * i + 1]);
+        }
+        const float tile_max = max3(max3(mx[0], mx[1], s[124]), max3(mx[2], mx[3], s[125]), fmaxf(s[126], s[127]));
         if (j == 0) {
           m = tile_max;
         } else if (__any_sync(0xffffffffu, (tile_max - m) * rs > kMaxSlack)) {
@@ -423,23 +447,31 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
         }
         const float shift = m == -INFINITY ? 0.f : m * rs;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        const float2 rs2 = make_float2(rs, rs), shift2 = make_float2(-shift, -shift);
 #pragma unroll
         for (int part = 0; part < 4; ++part) {
           uint32_t pk[16];
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
-            const float a = ex2(fmaf(s[32 * part + 2 * c], rs, -shift)), b = ex2(fmaf(s[32 * part + 2 * c + 1], rs, -shift));
-            sum[(2 * c) & 3] += a;
-            sum[(2 * c + 1) & 3] += b;
-            pk[c] = pack<kBf16>(a, b);
+            float2 e = fma2(make_float2(s[32 * part + 2 * c], s[32 * part + 2 * c + 1]), rs2, shift2);
+            e.x = ex2(e.x);
+            e.y = ex2(e.y);
+            sum[c & 1] = add2(sum[c & 1], e);
+            pk[c] = pack<kBf16>(e.x, e.y);
           }
           tmem_st16(s_tmem + 16 * part, pk);
+          if (part == kPEarly - 1) {   // the product starts on these while the rest is being worked out
+            wait_st();
+            fence_before();
+            arrive(bar(kBarP + t));
+          }
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        sum[0] = add2(sum[0], sum[1]);
+        l += sum[0].x + sum[0].y;
         wait_st();
         fence_before();
-        arrive(bar(kBarP + t));
+        arrive(bar(kBarPTail + t));
       }
       if (!ok) break;
       // ---- the result
@@ -652,10 +684,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         }
         commit(bar(kBarS + t));
       };
-      auto values = [&](int t, int v_stage, bool first) {   // O_t += P_t V
+      auto values = [&](int t, int v_stage, bool first, int k0, int k1) {   // O_t += P_t V, 16-token slices k0 .. k1 - 1
         const uint32_t b0 = desc_low(ring + v_stage * Shape::kTileBytes, kChunkKvTile * 128);
 #pragma unroll
-        for (int k = 0; k < kChunkKvTile / 16; ++k) {
+        for (int k = k0; k < k1; ++k) {
           mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, smem_desc(b0 + k * (2048 >> 4)), kDescO,
                  !(first && k == 0));
         }
@@ -675,9 +707,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             if (first) ok = next_tile(v_stage);
             ok = ok && wait(bar(kBarP + t), n_p[t] & 1, stop);
             if (!ok) break;
+            fence_after();
+            values(t, v_stage, i < 2, 0, 2 * kPEarly);
+            ok = wait(bar(kBarPTail + t), n_p[t] & 1, stop);
+            if (!ok) break;
             ++n_p[t];
             fence_after();
-            values(t, v_stage, i < 2);
+            values(t, v_stage, false, 2 * kPEarly, kChunkKvTile / 16);
             if (last) commit(bar(kBarEmpty + v_stage));
             if (i + 2 >= turns) commit(bar(kBarO + t));
           }
