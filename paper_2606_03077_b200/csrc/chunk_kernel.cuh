@@ -32,6 +32,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "chunk_plan.hpp"
 #include "libra.h"
@@ -67,6 +68,8 @@ struct ChunkShape {
   static constexpr int kRawBytes = kChunkKvTile * D;           // the same as E4M3 codes
   static constexpr int kStages = kFp8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);
   static constexpr int kRawStages = kFp8 ? (D == 128 ? 4 : 8) : 0;
+  // An item with one row tile leaves the second Q tile's place free: the ring is one stage longer then, and begins there.
+  static constexpr int kSoloStages = kStages < 8 ? kStages + 1 : kStages;
   static constexpr int kThreads = kFp8 ? 512 : 384;
   // registers a thread of each role: together what the launch brings (384 x 168, 512 x 128)
   static constexpr int kSoftmaxRegs = kFp8 ? 184 : 216, kIssueRegs = 72, kConvertRegs = 72;
@@ -298,11 +301,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   using namespace chunk;
   using Shape = ChunkShape<D, kFp8>;
   constexpr bool kBf16 = !kFp8;
-  constexpr int kStages = Shape::kStages;
   constexpr uint32_t kTmemColumns = 512;                  // S0 | S1 | O0 | O1, 128 columns each (O: D of them)
   extern __shared__ __align__(1024) uint8_t smem[];   // the 128-byte swizzle counts rows from 1024-byte boundaries
   const uint32_t base = smem_u32(smem);
-  const uint32_t q_tiles = base, ring = base + Shape::kRing, raw = base + Shape::kRaw;
+  const uint32_t q_tiles = base, raw = base + Shape::kRaw;
   float* const row_factor = reinterpret_cast<float*>(smem + Shape::kFloats);   // [2][128]
   float* const merge_ml = row_factor + 256;                                    // [2][128]
   auto bar = [&](int i) { return base + uint32_t(Shape::kBars + 8 * i); };
@@ -311,7 +313,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < Shape::kSoloStages; ++s) {
       mbar_init(bar(kBarFull + s), kFp8 ? 128 : 1);
       mbar_init(bar(kBarEmpty + s), 1);
     }
@@ -328,7 +330,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     }
     mbar_init(bar(kBarMergeFree), 128);
     mbar_init(bar(kBarMergeFull), 128);
-    mbar_init(bar(kBarMergeDone), 128);
     for (int i = 0; i < kLoaders; ++i) mbar_init(bar(kBarTail + i), 1);
     mbar_init(bar(kBarDrain), 1);
     fence_mbar_init();
@@ -344,6 +345,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   const uint32_t tmem = slots[2 * kSlotTmem];
   const bool run = slots[2 * kSlotStop] == 0;
   __syncthreads();   // every thread has read the stop flag before a role can set it
+  const bool solo = run && load_unit(p, blockIdx.x).solo;
+  const int n_stages = solo ? Shape::kSoloStages : Shape::kStages;
+  const uint32_t ring = base + Shape::kRing - uint32_t(n_stages - Shape::kStages) * Shape::kTileBytes;
 
   if (run && warp < 8) {
     // ------------------------------------------------------------------ softmax group t: row tile t (both: tile 0 if solo)
@@ -351,16 +355,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     const int t = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const uint32_t s_tmem = tmem + lanes + t * 128, o_tmem = tmem + lanes + 256 + t * 128;
-    uint32_t n_s = 0, n_q = 0, n_o = 0, n_solo = 0;   // phases seen
-    for (int u = blockIdx.x; u < p.num_units; u += gridDim.x) {
+    do {   // left by break when a wait has run out
       // what the steps need is kept, the rest of the item is read again where it is used: registers are short here
       int steps, all_steps, sees, kv0, kv_pitch;
-      bool solo;
       {
-        const ChunkUnit x = load_unit(p, u);
+        const ChunkUnit x = load_unit(p, blockIdx.x);
         all_steps = x.steps;
         steps = x.steps_of(t);
-        solo = x.solo;
         const int tile_row = (solo ? 0 : t * kChunkTileRows) + row;   // row within the item
         // cached tokens this row sees
         sees = tile_row < x.n_rows ? min(x.kv_end, x.ctx + (x.row0 + tile_row) / p.group + 1) : 0;
@@ -400,9 +401,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       arrive(bar(kBarQ + t));
       if constexpr (kFp8) {
         // the row factors come from the group that loaded the tile
-        if (!wait_warp(bar(kBarQ + (solo ? 0 : t)), n_q & 1, stop)) break;
+        if (!wait_warp(bar(kBarQ + (solo ? 0 : t)), 0, stop)) break;
       }
-      ++n_q;
       float rs = p.scale_log2;   // score -> base-2 exponent
       if constexpr (kFp8) {
         if (all_steps > 0) rs *= row_factor[(solo ? 0 : t) * 128 + row];
@@ -412,9 +412,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       bool ok = true;
 #pragma unroll 1
       for (int j = 0; j < steps; ++j, kv0 += kv_pitch) {
-        ok = wait_warp(bar(kBarS + t), n_s & 1, stop);
+        ok = wait_warp(bar(kBarS + t), j & 1, stop);
         if (!ok) break;
-        ++n_s;
         fence_after();
         float s[128];
 #pragma unroll
@@ -427,47 +426,64 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll
           for (int c = 0; c < 128; ++c) s[c] = c < limit ? s[c] : -INFINITY;
         }
-        float mx[4] = {s[0], s[1], s[2], s[3]};
+        auto row_max = [&] {
+          float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int c = 4; c < 124; c += 8) {
+          for (int c = 4; c < 124; c += 8) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], s[c + 2 * i], s[c + 2 * i + 1]);
-        }
-        const float tile_max = max3(max3(mx[0], mx[1], s[124]), max3(mx[2], mx[3], s[125]), fmaxf(s[126], s[127]));
-        if (j == 0) {
-          m = tile_max;
-        } else if (__any_sync(0xffffffffu, (tile_max - m) * rs > kMaxSlack)) {
-          // the product of the step before has finished: its completion comes before that of this step's scores
-          const float to = fmaxf(m, tile_max);
-          const float alpha = to == -INFINITY ? 1.f : ex2((m - to) * rs);
-          m = to;
-          l *= alpha;
-#pragma unroll
-          for (int c = 0; c < D; c += 16) {
-            float o[16];
-            tmem_ld16(o, o_tmem + c);
-            wait_ld();
-            settle<16>(o);
-            uint32_t scaled[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) scaled[i] = __float_as_uint(o[i] * alpha);
-            tmem_st16(o_tmem + c, scaled);
+            for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], s[c + 2 * i], s[c + 2 * i + 1]);
           }
-        }
-        const float shift = m == -INFINITY ? 0.f : m * rs;
-        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        const float2 rs2 = make_float2(rs, rs), shift2 = make_float2(-shift, -shift);
-#pragma unroll
-        for (int part = 0; part < 4; ++part) {
-          uint32_t pk[16];
+          return max3(max3(mx[0], mx[1], s[124]), max3(mx[2], mx[3], s[125]), fmaxf(s[126], s[127]));
+        };
+        if (j == 0) m = row_max();
+        float2 sum[2], shift2;
+        const float2 rs2 = make_float2(rs, rs);
+        uint32_t pk[16];
+        auto probabilities = [&](int part) {   // of 32 columns
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
             float2 e = fma2(make_float2(s[32 * part + 2 * c], s[32 * part + 2 * c + 1]), rs2, shift2);
             e.x = ex2(e.x);
             e.y = ex2(e.y);
-            sum[c & 1] = add2(sum[c & 1], e);
+            sum[c & 1] = part == 0 && c < 2 ? e : add2(sum[c & 1], e);
             pk[c] = pack<kBf16>(e.x, e.y);
           }
+        };
+        auto set_shift = [&] {
+          const float x = m == -INFINITY ? 0.f : -m * rs;
+          shift2 = make_float2(x, x);
+        };
+        // The first quarter goes by the running maximum as it stands, while this tile's maximum is being found: the
+        // exponentials keep their unit busy meanwhile.  It is done again where the maximum turns out to be too low.
+        set_shift();
+        probabilities(0);
+        const float tile_max = row_max();
+        if (__any_sync(0xffffffffu, (tile_max - m) * rs > kMaxSlack)) {
+          // the product of the step before has finished: its completion comes before that of this step's scores
+          const float to = fmaxf(m, tile_max);
+          const float alpha = to == -INFINITY ? 1.f : ex2((m - to) * rs);
+          m = to;
+          l *= alpha;
+          if (j > 0) {
+#pragma unroll
+            for (int c = 0; c < D; c += 16) {
+              float o[16];
+              tmem_ld16(o, o_tmem + c);
+              wait_ld();
+              settle<16>(o);
+              uint32_t scaled[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) scaled[i] = __float_as_uint(o[i] * alpha);
+              tmem_st16(o_tmem + c, scaled);
+            }
+          }
+          set_shift();
+          probabilities(0);
+        }
+        tmem_st16(s_tmem, pk);
+#pragma unroll
+        for (int part = 1; part < 4; ++part) {
+          probabilities(part);
           tmem_st16(s_tmem + 16 * part, pk);
           if (part == kPEarly - 1) {   // the product starts on these while the rest is being worked out
             wait_st();
@@ -484,8 +500,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       if (!ok) break;
       // ---- the result
       if (all_steps > 0) {
-        if (!wait_warp(bar(kBarO + t), n_o & 1, stop)) break;
-        ++n_o;
+        if (!wait_warp(bar(kBarO + t), 0, stop)) break;
         fence_after();
       }
       float w = 1.f;     // weight of this group's part
@@ -494,9 +509,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         float* const part = reinterpret_cast<float*>(smem);   // [D][128]
         if (t == 0) {
           arrive(bar(kBarMergeFree));
-          if (!wait_warp(bar(kBarMergeFull), n_solo & 1, stop)) break;
+          if (!wait_warp(bar(kBarMergeFull), 0, stop)) break;
         } else {
-          if (!wait_warp(bar(kBarMergeFree), n_solo & 1, stop)) break;
+          if (!wait_warp(bar(kBarMergeFree), 0, stop)) break;
           if (steps > 0) {
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
@@ -513,14 +528,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           merge_ml[row] = m;
           merge_ml[128 + row] = l;
           arrive(bar(kBarMergeFull));
-          // the tile is the next item's Q once every row of it has been read
-          if (!wait_warp(bar(kBarMergeDone), n_solo & 1, stop)) break;
         }
       }
-      if (solo && t == 1) {
-        n_solo += all_steps > 0;
-        continue;
-      }
+      if (solo && t == 1) break;   // group 0 writes the result
       float w1 = 0.f;
       if (solo && all_steps > 0) {
         const float m1 = merge_ml[row], l1 = merge_ml[128 + row];
@@ -532,7 +542,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       const float inv = l > 0.f ? p.v_scale / l : 0.f;
       const float lse = l > 0.f ? (m * rs + lg2(l)) * 0.6931471805599453f : (l == 0.f ? -INFINITY : l);
-      const ChunkUnit x = load_unit(p, u);
+      const ChunkUnit x = load_unit(p, blockIdx.x);
       const int tile_row = (solo ? 0 : t * kChunkTileRows) + row;
       const bool valid = tile_row < x.n_rows;
       const int token = (x.row0 + (valid ? tile_row : 0)) / p.group;
@@ -573,19 +583,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
         }
       }
-      if (solo && all_steps > 0) {
-        arrive(bar(kBarMergeDone));
-        if (!wait_warp(bar(kBarMergeDone), n_solo & 1, stop)) break;
-        ++n_solo;
-      }
-      fence_before();
-    }
+    } while (false);
   } else if (warp >= 8 && warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kIssueRegs));
     if (run && warp != 9) {
       // ------------------------------------------------------------------ copies
       const int loader = warp == 8 ? 0 : warp - 9;
-      constexpr int kN = kFp8 ? Shape::kRawStages : kStages;
+      const int n = kFp8 ? Shape::kRawStages : n_stages;
       constexpr int kFull = kFp8 ? kBarRawFull : kBarFull, kEmpty = kFp8 ? kBarRawEmpty : kBarEmpty;
       constexpr int kStageBytes = kFp8 ? Shape::kRawBytes : Shape::kTileBytes;
       constexpr int kBoxes = kFp8 ? 1 : D / 64;                     // per page
@@ -593,18 +597,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       const int tile_pages_shift = 7 - p.page_shift;                // 128 tokens are 8, 4 or 2 pages
       const int my_page = lane & ((1 << tile_pages_shift) - 1), my_box = lane >> tile_pages_shift;
       const int page_tokens = 1 << p.page_shift;
-      uint32_t n_tail = 0;
-      int first = 0, mine = loader;   // tiles of the ring before this item; the next tile that this warp brings
-      int stage = loader % kN;        // of tile `mine`
-      uint32_t phase = loader / kN;
+      const ChunkUnit x = load_unit(p, blockIdx.x);
+      uint32_t n_tail = 0, phase = 0;
+      int i = loader, stage = loader;   // the next tile that this warp brings, and its place (a ring has three stages or more)
       bool ok = true;
-      for (int u = blockIdx.x; ok && u < p.num_units; u += gridDim.x) {
-        const ChunkUnit x = load_unit(p, u);
-        const int end = first + 2 * x.steps;
-        if (mine >= end) {
-          first = end;
-          continue;
-        }
+      if (i < 2 * x.steps) {
         const int32_t* row = p.block_table + int64_t(x.b) * p.block_table_ld;
         // this lane's page of step j (every lane of a page holds its id); -1 past the range
         auto page_of = [&](int j) -> int32_t {
@@ -617,13 +614,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
           return id;
         };
-        int32_t next = page_of(x.step_of(mine - first));
-        for (; mine < end; mine += kLoaders) {
-          const int i = mine - first;
+        int32_t next = page_of(x.step_of(i));
+        for (; i < 2 * x.steps; i += kLoaders) {
           const bool is_v = x.is_v(i);
           const int left = x.kv_end - (x.kv_begin + x.step_of(i) * kChunkKvTile);   // live tokens from the tile's first on
           const int32_t page = next;
-          next = page_of(mine + kLoaders < end ? x.step_of(i + kLoaders) : x.steps);
+          next = page_of(i + kLoaders < 2 * x.steps ? x.step_of(i + kLoaders) : x.steps);
           const int pages = min(kChunkKvTile >> p.page_shift, (left + page_tokens - 1) >> p.page_shift);
           const bool tail = !kFp8 && is_v && left < kChunkKvTile;
           ok = wait_warp(bar(kEmpty + stage), phase ^ 1, stop);
@@ -655,16 +651,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             if (lane == 0) arrive(bar(kFull + stage));
           }
           stage += kLoaders;
-          if (stage >= kN) {
-            stage -= kN;
+          if (stage >= n) {
+            stage -= n;
             phase ^= 1;
           }
         }
-        first = end;
       }
       if (!ok) {   // leave no copy in flight behind: wait (bounded) for this warp's last fills
-        for (int g = mine - kLoaders; g >= 0 && g >= mine - kN; g -= kLoaders) {
-          for (int i = 0; i < 4096 && !mbar_try_wait(bar(kFull + g % kN), (g / kN) & 1); ++i) {}
+        for (int g = i - kLoaders; g >= 0 && g >= i - n; g -= kLoaders) {
+          for (int k = 0; k < 4096 && !mbar_try_wait(bar(kFull + g % n), (g / n) & 1); ++k) {}
         }
       }
     } else if (run && warp == 9) {
@@ -675,85 +670,105 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       constexpr uint32_t kDescS = instr_desc<kBf16>(kChunkKvTile, false), kDescO = instr_desc<kBf16>(D, true);
       const bool leader = elect_one();
       int stage = 0;
-      uint32_t phase = 0, n_q = 0, n_p = 0;   // n_p: bit t = parity of row tile t's probabilities
+      uint32_t phase = 0, n_p = 0;   // n_p: bit t = parity of row tile t's probabilities
       bool ok = true;
+      // What the instructions take is worked out ahead of the waits: between a wait and the instructions behind it nothing is
+      // computed, the tensor cores would stand still meanwhile.
+      const uint32_t ring_low = uniform(desc_low(ring, 0)), q_low = uniform(desc_low(q_tiles, 0));
+      const uint32_t tm = uniform(tmem);
+      constexpr uint32_t kTileLow = Shape::kTileBytes >> 4, kVLow = uint32_t((kChunkKvTile * 128) >> 4) << 16;   // lbo of V
       auto next_tile = [&](int& at) {   // the next tile of the ring, once it is there
         at = stage;
         if (!wait_warp(bar(kBarFull + stage), phase, stop)) return false;
-        if (++stage == kStages) {
+        if (++stage == n_stages) {
           stage = 0;
           phase ^= 1;
         }
-        fence_after();
         return true;
       };
-      auto scores = [&](int t, int q_tile, int k_stage) {   // S_t = Q K^T
-        const uint32_t a0 = uniform(desc_low(q_tiles + q_tile * Shape::kTileBytes, 0));
-        const uint32_t b0 = uniform(desc_low(ring + k_stage * Shape::kTileBytes, 0)), d = uniform(tmem + t * 128);
-        if (leader) {
+      auto scores = [&](int t, uint32_t a0, uint32_t b0) {   // S_t = Q K^T
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint32_t off = uint32_t((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
-            mma_ss(d, smem_desc(a0 + off), smem_desc(b0 + off), kDescS, k > 0);
-          }
-          commit(bar(kBarS + t));
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = uint32_t((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+          mma_ss(tm + t * 128, smem_desc(a0 + off), smem_desc(b0 + off), kDescS, k > 0);
         }
+        commit(bar(kBarS + t));
       };
-      auto values = [&](int t, int v_stage, bool first, int k0, int k1) {   // O_t += P_t V, 16-token slices k0 .. k1 - 1
-        const uint32_t b0 = uniform(desc_low(ring + v_stage * Shape::kTileBytes, kChunkKvTile * 128));
-        const uint32_t s0 = uniform(tmem + t * 128);
-        if (leader) {
+      auto values = [&](int t, uint32_t b0, bool first, int k0, int k1) {   // O_t += P_t V, 16-token slices k0 .. k1 - 1
 #pragma unroll
-          for (int k = k0; k < k1; ++k) mma_ts(s0 + 256, s0 + k * 8, smem_desc(b0 + k * (2048 >> 4)), kDescO, !(first && k == 0));
+        for (int k = k0; k < k1; ++k) {
+          mma_ts(tm + 256 + t * 128, tm + t * 128 + k * 8, smem_desc(b0 + k * (2048 >> 4)), kDescO, !(first && k == 0));
         }
       };
-      auto signal = [&](int b) {
-        if (leader) commit(bar(b));
-      };
-      for (int u = blockIdx.x; ok && u < p.num_units; u += gridDim.x) {
-        int turns, solo;
-        {
-          const ChunkUnit x = load_unit(p, u);
-          solo = uniform(int(x.solo));
-          turns = uniform(x.solo ? x.steps : 2 * x.steps);
-        }
-        ok = wait_warp(bar(kBarQ + 0), n_q & 1, stop) && wait_warp(bar(kBarQ + 1), n_q & 1, stop);
-        ++n_q;
-        if (!ok || turns == 0) continue;
+      int turns;
+      {
+        const ChunkUnit x = load_unit(p, blockIdx.x);
+        turns = uniform(solo ? x.steps : 2 * x.steps);
+      }
+      if (turns > 0 && wait_warp(bar(kBarQ + 0), 0, stop) && wait_warp(bar(kBarQ + 1), 0, stop)) {
         // turn i: pair: row tile i & 1 at step i / 2, the two share the tiles of K and V; solo: step i, row tile 0, group i & 1
-        int k_stage = 0, v_stage = 0;
+        auto take_turns = [&](auto is_solo) {
+          constexpr bool kSolo = decltype(is_solo)::value;
+          int k_stage = 0, v_stage = 0;
 #pragma unroll 1
-        for (int i0 = -2; ok && i0 < turns; i0 += 2) {
+          for (int i0 = -2; ok && i0 < turns; i0 += 2) {
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const int i = i0 + t;
-            const bool first = solo || t == 0, last = solo || t == 1;   // of the turns that use a tile
-            if (i0 >= 0 && i < turns) {
-              if (first) ok = ok && next_tile(v_stage);
-              ok = ok && wait_warp(bar(kBarP + t), (n_p >> t) & 1, stop);
+            for (int t = 0; t < 2; ++t) {
+              const int i = i0 + t;
+              const bool first = kSolo || t == 0, last = kSolo || t == 1;   // of the turns that use a tile
+              const bool now = i0 >= 0 && i < turns, more = i + 2 < turns;
+              if (first) {
+                if (now) ok = ok && next_tile(v_stage);
+                // an item with one row tile is bound by the copies: its next K is not worth waiting for before the product with V
+                if (more && !(kSolo && now)) ok = ok && next_tile(k_stage);
+              }
+              const uint32_t v_low = uniform(ring_low + kVLow + v_stage * kTileLow);
+              uint32_t k_low = uniform(ring_low + k_stage * kTileLow);
+              const uint32_t a_low = kSolo ? q_low : q_low + t * kTileLow;
+              if (now) {
+                ok = ok && wait_warp(bar(kBarP + t), (n_p >> t) & 1, stop);
+                if (!ok) break;
+                fence_after();
+                if (leader) values(t, v_low, i0 == 0, 0, 2 * kPEarly);
+                ok = wait_warp(bar(kBarPTail + t), (n_p >> t) & 1, stop);
+                n_p ^= 1u << t;
+              }
               if (!ok) break;
               fence_after();
-              values(t, v_stage, i0 == 0, 0, 2 * kPEarly);
-              ok = wait_warp(bar(kBarPTail + t), (n_p >> t) & 1, stop);
-              if (!ok) break;
-              n_p ^= 1u << t;
-              fence_after();
-              values(t, v_stage, false, 2 * kPEarly, kChunkKvTile / 16);
-              if (last) signal(kBarEmpty + v_stage);
-              if (i + 2 >= turns) signal(kBarO + t);
-            }
-            if (i + 2 < turns) {
-              if (first) ok = ok && next_tile(k_stage);
-              if (!ok) break;
-              scores(t, solo ? 0 : t, k_stage);
-              if (last) signal(kBarEmpty + k_stage);
+              if (kSolo && now) {
+                if (leader) {
+                  values(t, v_low, false, 2 * kPEarly, kChunkKvTile / 16);
+                  commit(bar(kBarEmpty + v_stage));
+                  if (!more) commit(bar(kBarO + t));
+                }
+                if (more) {
+                  ok = next_tile(k_stage);
+                  if (!ok) break;
+                  fence_after();
+                  k_low = uniform(ring_low + k_stage * kTileLow);
+                }
+              }
+              if (leader) {
+                if (now && !kSolo) {
+                  values(t, v_low, false, 2 * kPEarly, kChunkKvTile / 16);
+                  if (last) commit(bar(kBarEmpty + v_stage));
+                  if (!more) commit(bar(kBarO + t));
+                }
+                if (more) {
+                  scores(t, a_low, k_low);
+                  if (last) commit(bar(kBarEmpty + k_stage));
+                }
+              }
+              __syncwarp();
             }
           }
-        }
-        if (ok && turns == 1) signal(kBarO + 1);   // group 1 has no turn
+        };
+        if (solo) take_turns(std::true_type());
+        else take_turns(std::false_type());
+        if (ok && turns == 1 && leader) commit(bar(kBarO + 1));   // group 1 has no turn
       }
       if (!ok) {   // nothing may be in flight when the tensor memory is given back
-        signal(kBarDrain);
+        if (leader) commit(bar(kBarDrain));
         for (uint32_t i = 0; i < 4096 && !mbar_try_wait(bar(kBarDrain), 0); ++i) {}
       }
     }
@@ -765,13 +780,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         const int tid = threadIdx.x - 384;
         int stage = 0, rstage = 0;
         uint32_t phase = 0, rphase = 0;
-        bool ok = true;
-        for (int u = blockIdx.x; ok && u < p.num_units; u += gridDim.x) {
-          const ChunkUnit x = load_unit(p, u);
-          for (int i = 0; ok && i < 2 * x.steps; ++i) {
+        const ChunkUnit x = load_unit(p, blockIdx.x);
+        {
+          for (int i = 0; i < 2 * x.steps; ++i) {
             const int live = x.is_v(i) ? x.kv_end - (x.kv_begin + x.step_of(i) * kChunkKvTile) : kChunkKvTile;   // K needs no zeroing
-            ok = wait_warp(bar(kBarRawFull + rstage), rphase, stop) && wait_warp(bar(kBarEmpty + stage), phase ^ 1, stop);
-            if (!ok) break;
+            if (!wait_warp(bar(kBarRawFull + rstage), rphase, stop) || !wait_warp(bar(kBarEmpty + stage), phase ^ 1, stop)) break;
             const uint8_t* src = smem + Shape::kRaw + rstage * Shape::kRawBytes;
             const uint32_t dst = ring + stage * Shape::kTileBytes;
             constexpr int kVec = D / 16;   // 16-byte vectors of codes per token
@@ -793,7 +806,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             fence_proxy_async();
             arrive(bar(kBarFull + stage));
             arrive(bar(kBarRawEmpty + rstage));
-            if (++stage == kStages) { stage = 0; phase ^= 1; }
+            if (++stage == n_stages) { stage = 0; phase ^= 1; }
             if (++rstage == Shape::kRawStages) { rstage = 0; rphase ^= 1; }
           }
         }
