@@ -130,7 +130,7 @@ int libra_chunk_plan(libra_handle_t h, const int32_t* q_lens_host, const int32_t
   const size_t lse_off = merges_off + align_up(merges_bytes, 256);
   const size_t o_off = lse_off + align_up(rows * sizeof(float), 256);
   if (workspace_bytes < o_off + rows * h->cfg.head_dim * sizeof(float)) return LIBRA_WORKSPACE_TOO_SMALL;
-  if (int64_t(plan.items.size()) * h->cfg.num_kv_heads > 0x7fffffff) return LIBRA_UNSUPPORTED_SHAPE;
+  if (int64_t(plan.items.size()) > int64_t(65535) * 65535) return LIBRA_UNSUPPORTED_SHAPE;   // grid
 
   DeviceGuard guard(h->cfg.device);
   if (guard.err != cudaSuccess) return fail_cuda(h, guard.err);
@@ -224,10 +224,11 @@ int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const vo
   p.error_word = static_cast<uint32_t*>(error_word_dev);
   p.num_pages = h->cfg.num_pages;
   p.serial = c.serial;
-  p.num_units = c.n_items * h->cfg.num_kv_heads;
+  p.num_items = c.n_items;
   p.num_q_heads = h->cfg.num_q_heads;
   p.num_kv_heads = h->cfg.num_kv_heads;
   p.group = h->group;
+  p.group_inverse = uint32_t((65536 + h->group - 1) / h->group);
   p.block_table_ld = h->cfg.block_table_ld;
   p.page_shift = h->cfg.page_size == 16 ? 4 : (h->cfg.page_size == 32 ? 5 : 6);
   p.pos_head = c.pos_head;
@@ -237,7 +238,8 @@ int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const vo
   p.v_scale = h->v_scale;
   const int di = h->cfg.head_dim == 128 ? 1 : 0;
   const ChunkBuild& b = kBuilds[di][h->fp8 ? 1 : 0];
-  b.fn<<<unsigned(p.num_units), unsigned(b.threads), size_t(b.smem), st>>>(pm->map_k, pm->map_v, p);
+  const dim3 blocks(unsigned(p.num_kv_heads), unsigned(std::min(c.n_items, 65535)), unsigned((c.n_items + 65534) / 65535));
+  b.fn<<<blocks, unsigned(b.threads), size_t(b.smem), st>>>(pm->map_k, pm->map_v, p);
   LIBRA_CUDA_TRY(h, cudaGetLastError());
   ++h->launches;
   if (c.n_merges > 0) {

@@ -32,7 +32,6 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
-#include <type_traits>
 
 #include "chunk_plan.hpp"
 #include "libra.h"
@@ -53,8 +52,9 @@ struct ChunkParams {
   uint32_t* error_word;
   int64_t num_pages;
   uint32_t serial;
-  int32_t num_units;          // items x KV heads
+  int32_t num_items;
   int32_t num_q_heads, num_kv_heads, group;
+  uint32_t group_inverse;     // ceil(2^16 / group): v / group = v * group_inverse >> 16 for v < 4096
   int32_t block_table_ld;
   int32_t page_shift;
   int32_t pos_head, pos_page, pos_token;
@@ -96,21 +96,30 @@ constexpr int kLoaders = 3;   // warps 8, 10 and 11 take the ring's tiles by tur
 constexpr int kSlotStop = 48, kSlotTmem = 49;   // the stop flag and the tensor-memory address live in two more slots
 
 struct Stop {   // how a wait that ran out ends the block
-  volatile uint32_t* flag;
-  uint32_t* error_word;
+  uint32_t flag;                // shared-memory address
+  uint32_t* const& error_word;  // in the kernel's parameters
+  __device__ __forceinline__ bool set() const {
+    uint32_t v;
+    asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(v) : "r"(flag) : "memory");
+    return v != 0;
+  }
+  __device__ __forceinline__ void raise() const {
+    asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(flag), "r"(1u) : "memory");
+    atomicOr(error_word, uint32_t(LIBRA_ERR_WAIT_TIMEOUT));
+  }
 };
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, const Stop& stop) {
-  if (mbar_try_wait(bar, parity)) return true;
   for (uint32_t i = 0; i < kWaitLimit; ++i) {
     if (mbar_try_wait(bar, parity)) return true;
-    if (*stop.flag) return false;
+    if (stop.set()) return false;
   }
-  *stop.flag = 1;
-  atomicOr(stop.error_word, uint32_t(LIBRA_ERR_WAIT_TIMEOUT));
+  stop.raise();
   return false;
 }
+// The whole warp waits; in the usual case, the barrier is through already, with a single test.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const Stop& stop) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   return __all_sync(0xffffffffu, wait(bar, parity, stop));
 }
 __device__ __forceinline__ void arrive(uint32_t bar) {
@@ -281,12 +290,34 @@ __device__ __forceinline__ int4 load_again(const int4* at) {   // not merged wit
   asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at));
   return v;
 }
-__device__ __forceinline__ ChunkUnit load_unit(const ChunkParams& p, int u) {
-  const int4 a = load_again(p.items + 2 * (u / p.num_kv_heads)), c = load_again(p.items + 2 * (u / p.num_kv_heads) + 1);
+__device__ __forceinline__ uint32_t load_again(const uint32_t* at) {
+  uint32_t v;
+  asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(at));
+  return v;
+}
+__device__ __forceinline__ int item_of(const ChunkParams& p) { return min(int(blockIdx.y + blockIdx.z * 65535u), p.num_items - 1); }
+__device__ __forceinline__ void touch_unit(const ChunkParams& p) {
+  asm volatile("{\n\t.reg .b32 v;\n\tld.global.b32 v, [%0];\n\t}" ::"l"(p.items + 2 * item_of(p)));
+}
+// Row r of an item: its token within the sequence's chunk and its head within the group.  One division for the item's first
+// row, the rest by multiplication.
+struct RowMap {
+  int token0, rest;
+  __device__ __forceinline__ RowMap(const ChunkParams& p, int row0) : token0(row0 / p.group), rest(row0 - token0 * p.group) {}
+  __device__ __forceinline__ void at(const ChunkParams& p, int r, int& token, int& head) const {
+    const int v = rest + r, t = int((uint32_t(v) * p.group_inverse) >> 16);
+    token = token0 + t;
+    head = v - t * p.group;
+  }
+};
+// grid = (KV heads, items up to 65535, the rest by z): the heads of an item run side by side, they share its pages
+__device__ __forceinline__ ChunkUnit load_unit(const ChunkParams& p) {
+  const int item = item_of(p);
+  const int4 a = load_again(p.items + 2 * item), c = load_again(p.items + 2 * item + 1);
   ChunkUnit x;
   x.b = a.x; x.q_start = a.y; x.row0 = a.z; x.n_rows = a.w;
   x.kv_begin = c.x; x.kv_end = c.y; x.ctx = c.z; x.slot = c.w;
-  x.head = u % p.num_kv_heads;
+  x.head = blockIdx.x;
   x.steps = (x.kv_end - x.kv_begin + kChunkKvTile - 1) / kChunkKvTile;
   x.solo = x.n_rows <= kChunkTileRows;
   return x;
@@ -305,13 +336,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   extern __shared__ __align__(1024) uint8_t smem[];   // the 128-byte swizzle counts rows from 1024-byte boundaries
   const uint32_t base = smem_u32(smem);
   const uint32_t q_tiles = base, raw = base + Shape::kRaw;
-  float* const row_factor = reinterpret_cast<float*>(smem + Shape::kFloats);   // [2][128]
-  float* const merge_ml = row_factor + 256;                                    // [2][128]
   auto bar = [&](int i) { return base + uint32_t(Shape::kBars + 8 * i); };
-  volatile uint32_t* const slots = reinterpret_cast<volatile uint32_t*>(smem + Shape::kBars);
-  Stop stop{slots + 2 * kSlotStop, p.error_word};
+  const Stop stop{bar(kSlotStop), p.error_word};
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // The item is on its way into the L1 cache while the barriers and the tensor memory are being set up; each role then reads
+  // it for itself (kept in registers from here on it cost the roles' loops a spill and 5 % of the time).
+  const uint32_t found = load_again(p.serial_at);
+  touch_unit(p);
   if (threadIdx.x == 0) {
     for (int s = 0; s < Shape::kSoloStages; ++s) {
       mbar_init(bar(kBarFull + s), kFp8 ? 128 : 1);
@@ -333,19 +365,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     for (int i = 0; i < kLoaders; ++i) mbar_init(bar(kBarTail + i), 1);
     mbar_init(bar(kBarDrain), 1);
     fence_mbar_init();
-    // another plan in the workspace than the one this launch was made for: nothing is computed
-    const uint32_t found = *reinterpret_cast<const volatile uint32_t*>(p.serial_at);
-    slots[2 * kSlotStop] = found != p.serial ? 1u : 0u;
-    if (found != p.serial) atomicOr(p.error_word, uint32_t(LIBRA_ERR_PLAN_CHANGED));
+    *reinterpret_cast<volatile uint32_t*>(smem + Shape::kBars + 8 * kSlotStop) = 0;
   }
   if (warp == 9) tmem_alloc(bar(kSlotTmem), kTmemColumns);
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = slots[2 * kSlotTmem];
-  const bool run = slots[2 * kSlotStop] == 0;
-  __syncthreads();   // every thread has read the stop flag before a role can set it
-  const bool solo = run && load_unit(p, blockIdx.x).solo;
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + Shape::kBars + 8 * kSlotTmem);
+  // another plan in the workspace than the one this launch was made for: nothing is computed
+  const bool run = found == p.serial && blockIdx.y + blockIdx.z * 65535u < uint32_t(p.num_items);
+  if (found != p.serial && threadIdx.x == 0) atomicOr(p.error_word, uint32_t(LIBRA_ERR_PLAN_CHANGED));
+  const bool solo = load_unit(p).solo;
   const int n_stages = solo ? Shape::kSoloStages : Shape::kStages;
   const uint32_t ring = base + Shape::kRing - uint32_t(n_stages - Shape::kStages) * Shape::kTileBytes;
 
@@ -355,46 +385,44 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     const int t = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const uint32_t s_tmem = tmem + lanes + t * 128, o_tmem = tmem + lanes + 256 + t * 128;
+    float* const row_factor = reinterpret_cast<float*>(smem + Shape::kFloats);   // [2][128]
+    float* const merge_ml = row_factor + 256;                                    // [2][128]
     do {   // left by break when a wait has run out
-      // what the steps need is kept, the rest of the item is read again where it is used: registers are short here
-      int steps, all_steps, sees, kv0, kv_pitch;
+      ChunkUnit x = load_unit(p);
+      const RowMap rows(p, x.row0);
+      const int steps = x.steps_of(t), all_steps = x.steps;
+      const int kv_pitch = solo ? 2 * kChunkKvTile : kChunkKvTile;
+      int kv0 = x.kv_begin + (solo ? t * kChunkKvTile : 0), sees;
       {
-        const ChunkUnit x = load_unit(p, blockIdx.x);
-        all_steps = x.steps;
-        steps = x.steps_of(t);
         const int tile_row = (solo ? 0 : t * kChunkTileRows) + row;   // row within the item
-        // cached tokens this row sees
-        sees = tile_row < x.n_rows ? min(x.kv_end, x.ctx + (x.row0 + tile_row) / p.group + 1) : 0;
-        kv0 = x.kv_begin + (solo ? t * kChunkKvTile : 0);
-        kv_pitch = solo ? 2 * kChunkKvTile : kChunkKvTile;
-        // ---- Q: 16 lanes (8 at D = 64) bring one row
-        if (x.steps > 0 && !(x.solo && t == 1)) {
-          constexpr int kLanes = D / 8, kRowsAtOnce = 128 / kLanes, kBatch = 8;
-          const int c16 = row % kLanes;
-#pragma unroll 1
-          for (int r0 = row / kLanes; r0 < kChunkTileRows; r0 += kRowsAtOnce * kBatch) {
-            uint4 v[kBatch];
+        int token, head;
+        rows.at(p, tile_row, token, head);
+        sees = tile_row < x.n_rows ? min(x.kv_end, x.ctx + token + 1) : 0;   // cached tokens this row sees
+      }
+      // ---- Q: 16 threads (8 at D = 64) bring a row
+      if (all_steps > 0 && !(solo && t == 1)) {
+        constexpr int kLanes = D / 8, kRowsAtOnce = 128 / kLanes, kVecs = kChunkTileRows / kRowsAtOnce;
+        uint4 v[kVecs];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              const int ir = t * kChunkTileRows + r0 + i * kRowsAtOnce;
-              v[i] = make_uint4(0, 0, 0, 0);
-              if (ir < x.n_rows) {
-                const int flat = x.row0 + ir, tok = flat / p.group;
-                v[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (int64_t(x.q_start) + tok) * p.q_stride +
-                                                            int64_t(x.head * p.group + flat - tok * p.group) * D) + c16);
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              const int r = r0 + i * kRowsAtOnce;
-              if constexpr (kFp8) {
-                float down;
-                v[i] = scaled_half_row<kLanes>(v[i], down);
-                if (c16 == 0) row_factor[t * 128 + r] = down;
-              }
-              st_shared(q_tiles + t * Shape::kTileBytes + swizzled(r, c16), v[i]);
-            }
+        for (int i = 0; i < kVecs; ++i) {
+          const int ir = t * kChunkTileRows + row / kLanes + i * kRowsAtOnce;
+          v[i] = make_uint4(0, 0, 0, 0);
+          if (ir < x.n_rows) {
+            int token, head;
+            rows.at(p, ir, token, head);
+            v[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (int64_t(x.q_start) + token) * p.q_stride +
+                                                        int64_t(x.head * p.group + head) * D) + row % kLanes);
           }
+        }
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+          const int r = row / kLanes + i * kRowsAtOnce;
+          if constexpr (kFp8) {
+            float down;
+            v[i] = scaled_half_row<kLanes>(v[i], down);
+            if (row % kLanes == 0) row_factor[t * 128 + r] = down;
+          }
+          st_shared(q_tiles + t * Shape::kTileBytes + swizzled(r, row % kLanes), v[i]);
         }
       }
       fence_proxy_async();
@@ -498,7 +526,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         arrive(bar(kBarPTail + t));
       }
       if (!ok) break;
-      // ---- the result
+      // ---- the result.  Of the item only what the steps need was kept; it is read again while the last product ends.
+      x = load_unit(p);
       if (all_steps > 0) {
         if (!wait_warp(bar(kBarO + t), 0, stop)) break;
         fence_after();
@@ -542,12 +571,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       const float inv = l > 0.f ? p.v_scale / l : 0.f;
       const float lse = l > 0.f ? (m * rs + lg2(l)) * 0.6931471805599453f : (l == 0.f ? -INFINITY : l);
-      const ChunkUnit x = load_unit(p, blockIdx.x);
       const int tile_row = (solo ? 0 : t * kChunkTileRows) + row;
       const bool valid = tile_row < x.n_rows;
-      const int token = (x.row0 + (valid ? tile_row : 0)) / p.group;
-      const int q_head = x.head * p.group + (x.row0 + (valid ? tile_row : 0)) - token * p.group;
-      const int64_t out_row = (int64_t(x.q_start) + token) * p.num_q_heads + q_head;
+      int token, head;
+      RowMap(p, x.row0).at(p, valid ? tile_row : 0, token, head);
+      const int64_t out_row = (int64_t(x.q_start) + token) * p.num_q_heads + x.head * p.group + head;
       const int64_t part_row = (int64_t(x.slot) + tile_row) * p.num_kv_heads + x.head;
       if (valid) {
         if (x.slot >= 0) p.partial_lse[part_row] = lse;
@@ -597,7 +625,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       const int tile_pages_shift = 7 - p.page_shift;                // 128 tokens are 8, 4 or 2 pages
       const int my_page = lane & ((1 << tile_pages_shift) - 1), my_box = lane >> tile_pages_shift;
       const int page_tokens = 1 << p.page_shift;
-      const ChunkUnit x = load_unit(p, blockIdx.x);
+      const ChunkUnit x = load_unit(p);
       uint32_t n_tail = 0, phase = 0;
       int i = loader, stage = loader;   // the next tile that this warp brings, and its place (a ring has three stages or more)
       bool ok = true;
@@ -702,29 +730,26 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       };
       int turns;
       {
-        const ChunkUnit x = load_unit(p, blockIdx.x);
+        const ChunkUnit x = load_unit(p);
         turns = uniform(solo ? x.steps : 2 * x.steps);
       }
       if (turns > 0 && wait_warp(bar(kBarQ + 0), 0, stop) && wait_warp(bar(kBarQ + 1), 0, stop)) {
-        // turn i: pair: row tile i & 1 at step i / 2, the two share the tiles of K and V; solo: step i, row tile 0, group i & 1
-        auto take_turns = [&](auto is_solo) {
-          constexpr bool kSolo = decltype(is_solo)::value;
-          int k_stage = 0, v_stage = 0;
+        // Two kinds of items, two loops: written as one with the difference tested, either ran 3 - 8 % slower (the time between the
+        // end of a wait and the next product is what this warp is made of).  No __syncwarp: the votes of the waits suffice.
+        int k_stage = 0, v_stage = 0;
+        if (!solo) {   // turn i is row tile i & 1 at step i / 2; the two share the tiles of K and V
 #pragma unroll 1
           for (int i0 = -2; ok && i0 < turns; i0 += 2) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
               const int i = i0 + t;
-              const bool first = kSolo || t == 0, last = kSolo || t == 1;   // of the turns that use a tile
               const bool now = i0 >= 0 && i < turns, more = i + 2 < turns;
-              if (first) {
+              if (t == 0) {
                 if (now) ok = ok && next_tile(v_stage);
-                // an item with one row tile is bound by the copies: its next K is not worth waiting for before the product with V
-                if (more && !(kSolo && now)) ok = ok && next_tile(k_stage);
+                if (more) ok = ok && next_tile(k_stage);
               }
               const uint32_t v_low = uniform(ring_low + kVLow + v_stage * kTileLow);
-              uint32_t k_low = uniform(ring_low + k_stage * kTileLow);
-              const uint32_t a_low = kSolo ? q_low : q_low + t * kTileLow;
+              const uint32_t k_low = uniform(ring_low + k_stage * kTileLow);
               if (now) {
                 ok = ok && wait_warp(bar(kBarP + t), (n_p >> t) & 1, stop);
                 if (!ok) break;
@@ -735,36 +760,56 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
               }
               if (!ok) break;
               fence_after();
-              if (kSolo && now) {
-                if (leader) {
-                  values(t, v_low, false, 2 * kPEarly, kChunkKvTile / 16);
-                  commit(bar(kBarEmpty + v_stage));
-                  if (!more) commit(bar(kBarO + t));
-                }
-                if (more) {
-                  ok = next_tile(k_stage);
-                  if (!ok) break;
-                  fence_after();
-                  k_low = uniform(ring_low + k_stage * kTileLow);
-                }
-              }
               if (leader) {
-                if (now && !kSolo) {
+                if (now) {
                   values(t, v_low, false, 2 * kPEarly, kChunkKvTile / 16);
-                  if (last) commit(bar(kBarEmpty + v_stage));
+                  if (t == 1) commit(bar(kBarEmpty + v_stage));
                   if (!more) commit(bar(kBarO + t));
                 }
                 if (more) {
-                  scores(t, a_low, k_low);
-                  if (last) commit(bar(kBarEmpty + k_stage));
+                  scores(t, q_low + t * kTileLow, k_low);
+                  if (t == 1) commit(bar(kBarEmpty + k_stage));
                 }
               }
-              __syncwarp();
             }
           }
-        };
-        if (solo) take_turns(std::true_type());
-        else take_turns(std::false_type());
+        } else {   // turn i is step i of row tile 0, taken by group i & 1; bound by the copies: the next K is waited for last
+          auto signal = [&](int b) {
+            if (leader) commit(bar(b));
+          };
+#pragma unroll 1
+          for (int i0 = -2; ok && i0 < turns; i0 += 2) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const int i = i0 + t;
+              if (i0 >= 0 && i < turns) {
+                ok = ok && next_tile(v_stage);
+                fence_after();
+                ok = ok && wait_warp(bar(kBarP + t), (n_p >> t) & 1, stop);
+                if (!ok) break;
+                fence_after();
+                uint32_t v_low = uniform(ring_low + kVLow + v_stage * kTileLow);
+                if (leader) values(t, v_low, i0 == 0, 0, 2 * kPEarly);
+                ok = wait_warp(bar(kBarPTail + t), (n_p >> t) & 1, stop);
+                if (!ok) break;
+                n_p ^= 1u << t;
+                fence_after();
+                v_low = uniform(ring_low + kVLow + v_stage * kTileLow);
+                if (leader) values(t, v_low, false, 2 * kPEarly, kChunkKvTile / 16);
+                signal(kBarEmpty + v_stage);
+                if (i + 2 >= turns) signal(kBarO + t);
+              }
+              if (i + 2 < turns) {
+                ok = ok && next_tile(k_stage);
+                fence_after();
+                if (!ok) break;
+                const uint32_t k_low = uniform(ring_low + k_stage * kTileLow);
+                if (leader) scores(t, q_low, k_low);
+                signal(kBarEmpty + k_stage);
+              }
+            }
+          }
+        }
         if (ok && turns == 1 && leader) commit(bar(kBarO + 1));   // group 1 has no turn
       }
       if (!ok) {   // nothing may be in flight when the tensor memory is given back
@@ -780,7 +825,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         const int tid = threadIdx.x - 384;
         int stage = 0, rstage = 0;
         uint32_t phase = 0, rphase = 0;
-        const ChunkUnit x = load_unit(p, blockIdx.x);
+        const ChunkUnit x = load_unit(p);
         {
           for (int i = 0; i < 2 * x.steps; ++i) {
             const int live = x.is_v(i) ? x.kv_end - (x.kv_begin + x.step_of(i) * kChunkKvTile) : kChunkKvTile;   // K needs no zeroing
