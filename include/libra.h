@@ -501,7 +501,7 @@ int libra_rope_init(libra_rope_t* rope, int32_t rotary_dim, int32_t layout, doub
  * (t, h, c) at t * stride_token + h * stride_head + c; positions is int32[n_tokens] on the device.  direction
  * LIBRA_ROPE_FORWARD is the map above; LIBRA_ROPE_GRADIENT is its transpose, which takes the gradient of the output to the
  * gradient of the input (magnitude included).  out may be x (with the same strides); any other overlap is not allowed.
- * Arithmetic in float32, one rounding to `dtype`.  head_dim is even, rotary_dim <= head_dim <= 1024; rows need no more than the
+ * Arithmetic in float32, one rounding to `dtype`.  head_dim is even, rotary_dim <= head_dim <= 1024, n_heads <= 16384; rows need no more than the
  * element's own alignment (16-byte aligned ones are faster).  Asynchronous on `stream`; nothing is allocated.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE, CUDA_ERROR. */
 #define LIBRA_ROPE_BF16 0
@@ -529,7 +529,7 @@ int libra_rope_apply(int32_t device, const libra_rope_t* rope, const void* x, vo
  * multiples of 8; no two rows of a call may name the same slot.  Bits of *error_word_dev (32-bit device word):
  * LIBRA_ERR_BAD_PAGE_ID for a page id outside the pool, LIBRA_ERR_PLAN_OVERFLOW for a token past the end of a block-table
  * row; such a token is not stored.  The handle supplies the pool geometry and type; no plan, no workspace.  Asynchronous on
- * `stream`.  Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (rotary_dim > head_dim), CUDA_ERROR. */
+ * `stream`.  Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (rotary_dim > head_dim; more than 16384 heads together), CUDA_ERROR. */
 int libra_rope_append(libra_handle_t handle, const libra_rope_t* rope, const void* q, int64_t q_stride, void* q_out,
                       int64_t q_out_stride, const void* k_new, const void* v_new, int64_t kv_stride,
                       const int32_t* q_offsets, const int32_t* seq_lens, const int32_t* block_table, int32_t batch,

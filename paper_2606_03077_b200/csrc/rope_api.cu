@@ -20,6 +20,10 @@ bool valid_rope(const libra_rope_t* r) {   // a struct that libra_rope_init fill
          (r->layout == LIBRA_ROPE_HALF || r->layout == LIBRA_ROPE_INTERLEAVED);
 }
 
+constexpr int kMaxHeads = 16384;   // a block's rows are divided by the heads with one 32-bit multiplication
+
+uint32_t inverse(int heads) { return uint32_t(((uint64_t(1) << 32) + heads - 1) / heads); }
+
 // Tokens per block: as many as share the block's threads in the sine and cosine pass (one evaluation per thread), fewer
 // when that would leave multiprocessors without a block.
 int tokens_per_block(int64_t tokens, int pairs, int n_sm) {
@@ -56,7 +60,7 @@ int libra_rope_apply(int32_t device, const libra_rope_t* rope, const void* x, vo
   if ((n_tokens > 1 && out_stride_token < head_dim) || (n_heads > 1 && out_stride_head < head_dim)) return LIBRA_INVALID_ARGUMENT;
   if (x == out && (x_stride_token != out_stride_token || x_stride_head != out_stride_head)) return LIBRA_INVALID_ARGUMENT;
   if (head_dim % 2 != 0 || head_dim > 1024 || rope->rotary_dim > head_dim) return LIBRA_UNSUPPORTED_SHAPE;
-  if (int64_t(n_heads) * head_dim > (int64_t(1) << 24) || n_tokens > 0x7fffffff) return LIBRA_UNSUPPORTED_SHAPE;
+  if (n_heads > kMaxHeads || n_tokens > 0x7fffffff) return LIBRA_UNSUPPORTED_SHAPE;
   const int eb = dtype == LIBRA_ROPE_F32 ? 4 : 2;
   if (!aligned(x, eb) || !aligned(out, eb) || !aligned(positions, 4)) return LIBRA_INVALID_ARGUMENT;
   if (n_tokens == 0) return LIBRA_OK;
@@ -77,6 +81,7 @@ int libra_rope_apply(int32_t device, const libra_rope_t* rope, const void* x, vo
   p.n_tokens = n_tokens;
   p.n_heads = n_heads;
   p.head_dim = head_dim;
+  p.heads_inverse = inverse(n_heads);
   p.gradient = direction == LIBRA_ROPE_GRADIENT;
   p.rope = *rope;
   const int pairs = rope->rotary_dim / 2;
@@ -116,7 +121,8 @@ int libra_rope_append(libra_handle_t h, const libra_rope_t* rope, const void* q,
     return LIBRA_INVALID_ARGUMENT;
   }
   if (rope && rope->rotary_dim > D) return LIBRA_UNSUPPORTED_SHAPE;
-  if (q_row + 2 * kv_row > (int64_t(1) << 24)) return LIBRA_UNSUPPORTED_SHAPE;
+  const int heads = (q ? h->cfg.num_q_heads : 0) + 2 * h->cfg.num_kv_heads;
+  if (heads > kMaxHeads) return LIBRA_UNSUPPORTED_SHAPE;
   if (batch == 0 || max_rows == 0) return LIBRA_OK;
   DeviceGuard guard(h->cfg.device);
   if (guard.err != cudaSuccess) return fail_cuda(h, guard.err);
@@ -148,6 +154,8 @@ int libra_rope_append(libra_handle_t h, const libra_rope_t* rope, const void* q,
   p.num_q_heads = h->cfg.num_q_heads;
   p.num_kv_heads = h->cfg.num_kv_heads;
   p.head_dim = D;
+  p.heads = heads;
+  p.heads_inverse = inverse(heads);
   if (rope) p.rope = *rope;
   else p.rope = libra_rope_t{};   // rotary_dim 0: every channel passes through
   const int pairs = p.rope.rotary_dim / 2;

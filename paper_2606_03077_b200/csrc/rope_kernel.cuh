@@ -25,7 +25,8 @@
 namespace libra {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeMaxTokens = 8;   // tokens per block at most
+constexpr int kRopeMaxTokens = 4;   // tokens per block at most: with 8 a block is too long, with 2 the sines weigh (43.9, 41.6 and
+                                    // 45.7 us for 2, 4, 8 tokens: 8191 tokens of 40 heads, 64 of 128 channels rotated)
 
 namespace rope {
 
@@ -84,6 +85,32 @@ __host__ __device__ __forceinline__ int items_per_head(int rotary_dim, int head_
   return rotating_items<V, kHalf>(rotary_dim) + (head_dim - rotary_dim) / V;
 }
 
+// A thread keeps one item j and walks over rows (token, head): no division but one multiplication per row.
+struct Walk {
+  int j;      // item
+  int first;  // first row
+  int step;   // rows between this thread's rows
+  __device__ __forceinline__ explicit Walk(int per_head) {
+    step = kRopeThreads / per_head;          // 0: a head has more items than the block has threads
+    if (step > 0) {
+      first = int(threadIdx.x) / per_head;
+      j = int(threadIdx.x) - first * per_head;
+      if (first >= step) first = 0x3fffffff;   // threads behind the last whole head
+    } else {
+      first = 0;
+      step = 1;
+      j = threadIdx.x;
+    }
+  }
+};
+// The factors of a token's pairs are laid out for items of V pairs (V / 2, interleaved): the same pair of neighbouring items
+// side by side.
+template <int V, bool kHalf>
+__device__ __forceinline__ int factor_at(int pair, int pairs) {
+  constexpr int kPer = kHalf ? V : V / 2;
+  return (pair % kPer) * (pairs / kPer) + pair / kPer;
+}
+
 }  // namespace rope
 
 struct RopeApplyParams {
@@ -94,6 +121,7 @@ struct RopeApplyParams {
   int64_t n_tokens;
   int32_t n_heads, head_dim;
   int32_t tokens_per_block;
+  uint32_t heads_inverse;   // ceil(2^32 / n_heads): row / n_heads = the upper word of the product, for kRopeMaxTokens * n_heads rows
   int32_t gradient;
   libra_rope_t rope;
 };
@@ -109,50 +137,66 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const __grid_c
     const int tok = i / pairs, pr = i - tok * pairs;
     float2 f = rope::cos_sin(__ldg(p.positions + t0 + tok), p.rope.turns[pr], p.rope.magnitude);
     if (p.gradient) f.y = -f.y;
-    cs[i] = f;
+    cs[tok * pairs + rope::factor_at<V, kHalf>(pr, pairs)] = f;
   }
   __syncthreads();
   const int rot = rope::rotating_items<V, kHalf>(p.rope.rotary_dim);
   const int per_head = rope::items_per_head<V, kHalf>(p.rope.rotary_dim, p.head_dim);
-  const int per_token = per_head * p.n_heads;
   const bool in_place = p.x == p.out;
-  for (int i = threadIdx.x; i < nt * per_token; i += kRopeThreads) {
-    const int tok = i / per_token, in_tok = i - tok * per_token;
-    const int head = in_tok / per_head, j = in_tok - head * per_head;
-    const T* src = static_cast<const T*>(p.x) + (t0 + tok) * p.x_stride_token + head * p.x_stride_head;
-    T* dst = static_cast<T*>(p.out) + (t0 + tok) * p.out_stride_token + head * p.out_stride_head;
-    alignas(16) T a[V];
-    if (j >= rot) {   // passes through
-      if (in_place) continue;
-      const int c = p.rope.rotary_dim + (j - rot) * V;
-      rope::load<T, V, kVector>(src + c, a);
-      rope::store<T, V, kVector>(dst + c, a);
-      continue;
-    }
-    const float2* f = cs + tok * pairs;
-    if constexpr (kHalf) {
-      alignas(16) T b[V];
-      rope::load<T, V, kVector>(src + j * V, a);
-      rope::load<T, V, kVector>(src + pairs + j * V, b);
+  const rope::Walk walk(per_head);
+  const int rows = nt * p.n_heads;
+  constexpr int kAtOnce = kVector && kHalf ? 1 : 2;   // rows whose loads are in flight together (twice as many: 5 - 8 % slower)
+  for (int j = walk.j; j < per_head; j += kRopeThreads) {
+    const bool turns = j < rot;
+    if (!turns && in_place) continue;
+    const int c = turns ? j * V : p.rope.rotary_dim + (j - rot) * V;
+    for (int r0 = walk.first; r0 < rows; r0 += kAtOnce * walk.step) {
+      alignas(16) T a[kAtOnce][V];
+      alignas(16) T b[kAtOnce][V];
+      int64_t dst[kAtOnce];
+      int tok[kAtOnce];
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const float2 w = f[j * V + k];
-        const float x = rope::to_f32(a[k]), y = rope::to_f32(b[k]);
-        a[k] = rope::from_f32<T>(x * w.x - y * w.y);
-        b[k] = rope::from_f32<T>(x * w.y + y * w.x);
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int row = r0 + u * walk.step;
+        tok[u] = -1;
+        if (row < rows) {
+          tok[u] = int(__umulhi(uint32_t(row), p.heads_inverse));
+          if (p.n_heads == 1) tok[u] = row;
+          const int head = row - tok[u] * p.n_heads;
+          const T* src = static_cast<const T*>(p.x) + (t0 + tok[u]) * p.x_stride_token + head * p.x_stride_head + c;
+          dst[u] = (t0 + tok[u]) * p.out_stride_token + head * p.out_stride_head + c;
+          rope::load<T, V, kVector>(src, a[u]);
+          if (kHalf && turns) rope::load<T, V, kVector>(src + pairs, b[u]);
+        }
       }
-      rope::store<T, V, kVector>(dst + j * V, a);
-      rope::store<T, V, kVector>(dst + pairs + j * V, b);
-    } else {
-      rope::load<T, V, kVector>(src + j * V, a);
 #pragma unroll
-      for (int k = 0; k < V; k += 2) {
-        const float2 w = f[(j * V + k) / 2];
-        const float x = rope::to_f32(a[k]), y = rope::to_f32(a[k + 1]);
-        a[k] = rope::from_f32<T>(x * w.x - y * w.y);
-        a[k + 1] = rope::from_f32<T>(x * w.y + y * w.x);
+      for (int u = 0; u < kAtOnce; ++u) {
+        if (tok[u] < 0) continue;
+        T* to = static_cast<T*>(p.out) + dst[u];
+        if (turns) {
+          const float2* f = cs + tok[u] * pairs + j;
+          const int pitch = rot;   // pairs / (V or V / 2)
+          if constexpr (kHalf) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+              const float2 w = f[k * pitch];
+              const float x = rope::to_f32(a[u][k]), y = rope::to_f32(b[u][k]);
+              a[u][k] = rope::from_f32<T>(x * w.x - y * w.y);
+              b[u][k] = rope::from_f32<T>(x * w.y + y * w.x);
+            }
+            rope::store<T, V, kVector>(to + pairs, b[u]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < V; k += 2) {
+              const float2 w = f[(k / 2) * pitch];
+              const float x = rope::to_f32(a[u][k]), y = rope::to_f32(a[u][k + 1]);
+              a[u][k] = rope::from_f32<T>(x * w.x - y * w.y);
+              a[u][k + 1] = rope::from_f32<T>(x * w.y + y * w.x);
+            }
+          }
+        }
+        rope::store<T, V, kVector>(to, a[u]);
       }
-      rope::store<T, V, kVector>(dst + j * V, a);
     }
   }
 }
@@ -176,6 +220,8 @@ struct RopeAppendParams {
   int32_t block_table_ld, page_shift;
   int32_t num_q_heads, num_kv_heads, head_dim;
   int32_t tokens_per_block;
+  int32_t heads;            // rows of a token: query heads (0 without q), then KV heads of k, then of v
+  uint32_t heads_inverse;   // as above, for kRopeMaxTokens * heads rows
   libra_rope_t rope;
 };
 
@@ -248,72 +294,88 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
   __syncthreads();
   for (int i = threadIdx.x; i < nt * pairs; i += kRopeThreads) {
     const int tok = i / pairs, pr = i - tok * pairs;
-    cs[i] = rope::cos_sin(s_pos[tok], p.rope.turns[pr], p.rope.magnitude);
+    cs[tok * pairs + rope::factor_at<V, kHalf>(pr, pairs)] = rope::cos_sin(s_pos[tok], p.rope.turns[pr], p.rope.magnitude);
   }
   __syncthreads();
   const int rot = rope::rotating_items<V, kHalf>(p.rope.rotary_dim);
   const int per_head = rope::items_per_head<V, kHalf>(p.rope.rotary_dim, p.head_dim);
-  const int v_per_head = p.head_dim / V;
-  const int q_heads = p.q ? p.num_q_heads : 0;
-  const int qk_items = (q_heads + p.num_kv_heads) * per_head;
-  const int per_token = qk_items + p.num_kv_heads * v_per_head;
-  for (int i = threadIdx.x; i < nt * per_token; i += kRopeThreads) {
-    const int tok = i / per_token, in_tok = i - tok * per_token;
-    const int64_t row = t0 + tok, slot = s_slot[tok];
-    if (slot == -2) continue;   // a row behind the last sequence
-    alignas(16) __nv_bfloat16 a[V];
-    float x[V];
-    if (in_tok >= qk_items) {   // a value row: copied
-      if (slot < 0) continue;
-      const int head = (in_tok - qk_items) / v_per_head, c = (in_tok - qk_items - head * v_per_head) * V;
-      rope::load<__nv_bfloat16, V, kVector>(p.v_new + row * p.kv_stride + head * p.head_dim + c, a);
+  const int q_heads = p.heads - 2 * p.num_kv_heads;
+  const rope::Walk walk(per_head);
+  const int rows = nt * p.heads;
+  constexpr int kAtOnce = kVector ? (kHalf ? 2 : 4) : 2;   // rows whose loads are in flight together (half: 4 % slower, twice: up to 60 %)
+  for (int j = walk.j; j < per_head; j += kRopeThreads) {
+    const bool turns = j < rot;
+    const int c = turns ? j * V : p.rope.rotary_dim + (j - rot) * V;
+    for (int r0 = walk.first; r0 < rows; r0 += kAtOnce * walk.step) {
+      alignas(16) __nv_bfloat16 a[kAtOnce][V];
+      alignas(16) __nv_bfloat16 b[kAtOnce][V];
+      int tok[kAtOnce], head[kAtOnce];
 #pragma unroll
-      for (int k = 0; k < V; ++k) x[k] = __bfloat162float(a[k]);
-      rope::store_pool<P, V, kVector>(static_cast<P*>(p.v_pool) + slot + head * p.stride_head + c, x, p.v_inv_scale);
-      continue;
-    }
-    const int head = in_tok / per_head, j = in_tok - head * per_head;
-    const bool is_q = head < q_heads;
-    if (!is_q && slot < 0) continue;
-    const __nv_bfloat16* src = is_q ? p.q + row * p.q_stride + head * p.head_dim
-                                    : p.k_new + row * p.kv_stride + (head - q_heads) * p.head_dim;
-    __nv_bfloat16* q_dst = p.q_out + row * p.q_out_stride + head * p.head_dim;                                   // if is_q
-    P* k_dst = static_cast<P*>(p.k_pool) + slot + (head - q_heads) * p.stride_head;                              // else
-    auto put = [&](int c, const float (&y)[V]) {
-      if (is_q) rope::store_pool<__nv_bfloat16, V, kVector>(q_dst + c, y, 1.f);
-      else rope::store_pool<P, V, kVector>(k_dst + c, y, p.k_inv_scale);
-    };
-    const float2* f = cs + tok * pairs;
-    if (j >= rot) {
-      const int c = p.rope.rotary_dim + (j - rot) * V;
-      rope::load<__nv_bfloat16, V, kVector>(src + c, a);
-#pragma unroll
-      for (int k = 0; k < V; ++k) x[k] = __bfloat162float(a[k]);
-      put(c, x);
-    } else if constexpr (kHalf) {
-      alignas(16) __nv_bfloat16 b[V];
-      float y[V];
-      rope::load<__nv_bfloat16, V, kVector>(src + j * V, a);
-      rope::load<__nv_bfloat16, V, kVector>(src + pairs + j * V, b);
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const float2 w = f[j * V + k];
-        const float u = __bfloat162float(a[k]), v = __bfloat162float(b[k]);
-        x[k] = u * w.x - v * w.y;
-        y[k] = u * w.y + v * w.x;
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int row = r0 + u * walk.step;
+        tok[u] = -1;
+        if (row < rows) {
+          tok[u] = int(__umulhi(uint32_t(row), p.heads_inverse));
+          head[u] = row - tok[u] * p.heads;
+          const int64_t slot = s_slot[tok[u]];
+          // a row behind the last sequence; a key or value that is not stored
+          if (slot == -2 || (slot < 0 && head[u] >= q_heads)) {
+            tok[u] = -1;
+          } else {
+            const int64_t at = t0 + tok[u];
+            const __nv_bfloat16* src =
+                head[u] < q_heads ? p.q + at * p.q_stride + head[u] * p.head_dim
+                : head[u] < q_heads + p.num_kv_heads ? p.k_new + at * p.kv_stride + (head[u] - q_heads) * p.head_dim
+                                                     : p.v_new + at * p.kv_stride + (head[u] - q_heads - p.num_kv_heads) * p.head_dim;
+            rope::load<__nv_bfloat16, V, kVector>(src + c, a[u]);
+            if (kHalf && turns) rope::load<__nv_bfloat16, V, kVector>(src + c + pairs, b[u]);
+          }
+        }
       }
-      put(j * V, x);
-      put(pairs + j * V, y);
-    } else {
-      rope::load<__nv_bfloat16, V, kVector>(src + j * V, a);
 #pragma unroll
-      for (int k = 0; k < V; k += 2) {
-        const float2 w = f[(j * V + k) / 2];
-        const float u = __bfloat162float(a[k]), v = __bfloat162float(a[k + 1]);
-        x[k] = u * w.x - v * w.y;
-        x[k + 1] = u * w.y + v * w.x;
+      for (int u = 0; u < kAtOnce; ++u) {
+        if (tok[u] < 0) continue;
+        const bool is_q = head[u] < q_heads, is_v = head[u] >= q_heads + p.num_kv_heads;
+        float x[V], y[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) x[k] = __bfloat162float(a[u][k]);
+        if (kHalf && turns) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) y[k] = __bfloat162float(b[u][k]);
+        }
+        if (turns && !is_v) {
+          const float2* f = cs + tok[u] * pairs + j;
+          const int pitch = rot;   // pairs / (V or V / 2)
+          if constexpr (kHalf) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+              const float2 w = f[k * pitch];
+              const float s = x[k], t = y[k];
+              x[k] = s * w.x - t * w.y;
+              y[k] = s * w.y + t * w.x;
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < V; k += 2) {
+              const float2 w = f[(k / 2) * pitch];
+              const float s = x[k], t = x[k + 1];
+              x[k] = s * w.x - t * w.y;
+              x[k + 1] = s * w.y + t * w.x;
+            }
+          }
+        }
+        if (is_q) {
+          __nv_bfloat16* to = p.q_out + int64_t(t0 + tok[u]) * p.q_out_stride + head[u] * p.head_dim + c;
+          rope::store_pool<__nv_bfloat16, V, kVector>(to, x, 1.f);
+          if (kHalf && turns) rope::store_pool<__nv_bfloat16, V, kVector>(to + pairs, y, 1.f);
+        } else {
+          const int kv_head = head[u] - q_heads - (is_v ? p.num_kv_heads : 0);
+          P* to = static_cast<P*>(is_v ? p.v_pool : p.k_pool) + s_slot[tok[u]] + kv_head * p.stride_head + c;
+          const float inv = is_v ? p.v_inv_scale : p.k_inv_scale;
+          rope::store_pool<P, V, kVector>(to, x, inv);
+          if (kHalf && turns) rope::store_pool<P, V, kVector>(to + pairs, y, inv);
+        }
       }
-      put(j * V, x);
     }
   }
 }
