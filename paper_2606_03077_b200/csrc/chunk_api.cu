@@ -42,6 +42,22 @@ uint32_t next_serial() {
   return n;
 }
 
+// As a programmatic dependent of its predecessor where the handle allows it; the kernels wait for that one inside.
+template <typename... P, typename... A>
+cudaError_t launch(bool dependent, void (*fn)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = grid;
+  lc.blockDim = dim3(threads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = attr;
+  lc.numAttrs = dependent ? 1 : 0;
+  return cudaLaunchKernelEx(&lc, fn, args...);
+}
+
 int set_attributes(libra_handle_t h) {
   if (h->chunk.attributes_set) return LIBRA_OK;
   for (const auto& row : kBuilds) {
@@ -239,8 +255,7 @@ int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const vo
   const int di = h->cfg.head_dim == 128 ? 1 : 0;
   const ChunkBuild& b = kBuilds[di][h->fp8 ? 1 : 0];
   const dim3 blocks(unsigned(p.num_kv_heads), unsigned(std::min(c.n_items, 65535)), unsigned((c.n_items + 65534) / 65535));
-  b.fn<<<blocks, unsigned(b.threads), size_t(b.smem), st>>>(pm->map_k, pm->map_v, p);
-  LIBRA_CUDA_TRY(h, cudaGetLastError());
+  LIBRA_CUDA_TRY(h, launch(h->pdl, b.fn, blocks, unsigned(b.threads), size_t(b.smem), st, pm->map_k, pm->map_v, p));
   ++h->launches;
   if (c.n_merges > 0) {
     libra::ChunkMergeParams m;
@@ -255,9 +270,8 @@ int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const vo
     m.num_kv_heads = p.num_kv_heads;
     m.group = p.group;
     const dim3 grid(unsigned(c.n_merges * p.num_kv_heads), unsigned(libra::kChunkItemRows / libra::kChunkMergeWarps));
-    if (di) libra::chunk_merge_kernel<128><<<grid, libra::kChunkMergeWarps * 32, 0, st>>>(m);
-    else libra::chunk_merge_kernel<64><<<grid, libra::kChunkMergeWarps * 32, 0, st>>>(m);
-    LIBRA_CUDA_TRY(h, cudaGetLastError());
+    LIBRA_CUDA_TRY(h, launch(h->pdl, di ? libra::chunk_merge_kernel<128> : libra::chunk_merge_kernel<64>, grid,
+                             unsigned(libra::kChunkMergeWarps * 32), 0, st, m));
     ++h->launches;
   }
   return LIBRA_OK;

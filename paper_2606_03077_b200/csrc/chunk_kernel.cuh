@@ -89,8 +89,8 @@ namespace chunk {
 using namespace dev;
 
 // barriers, in 8-byte slots after the floats
-constexpr int kBarFull = 0, kBarEmpty = 8, kBarRawFull = 16, kBarRawEmpty = 24, kBarQ = 32, kBarS = 34, kBarP = 36, kBarO = 38, kBarPTail = 50,
-              kBarMergeFree = 40, kBarMergeFull = 41, kBarMergeDone = 42, kBarDrain = 43, kBarTail = 44;
+constexpr int kBarFull = 0, kBarEmpty = 8, kBarRawFull = 16, kBarRawEmpty = 24, kBarQ = 32, kBarS = 34, kBarP = 36, kBarPTail = 38,
+              kBarO = 40, kBarMergeFree = 42, kBarMergeFull = 43, kBarDrain = 44, kBarTail = 45, kNumBars = 48;
 constexpr int kPEarly = 3;    // quarters of a step's probabilities that the second product starts on
 constexpr int kLoaders = 3;   // warps 8, 10 and 11 take the ring's tiles by turns
 constexpr int kSlotStop = 48, kSlotTmem = 49;   // the stop flag and the tensor-memory address live in two more slots
@@ -272,6 +272,12 @@ __device__ __forceinline__ uint4 scaled_half_row(uint4 v, float& down) {
   return make_uint4(h[0], h[1], h[2], h[3]);
 }
 
+__device__ __forceinline__ uint4 ld_shared(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 // One unit of work as every role sees it.
 struct ChunkUnit {
   int b, q_start, row0, n_rows, kv_begin, kv_end, ctx, slot;
@@ -340,32 +346,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   const Stop stop{bar(kSlotStop), p.error_word};
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // launched as a dependent of whatever precedes it in the stream
   // The item is on its way into the L1 cache while the barriers and the tensor memory are being set up; each role then reads
   // it for itself (kept in registers from here on it cost the roles' loops a spill and 5 % of the time).
   const uint32_t found = load_again(p.serial_at);
   touch_unit(p);
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < Shape::kSoloStages; ++s) {
-      mbar_init(bar(kBarFull + s), kFp8 ? 128 : 1);
-      mbar_init(bar(kBarEmpty + s), 1);
+  if (warp == 0) {   // the barriers, two a lane; what arrives on each: one instruction or copy, or the 128 threads of a group
+    for (int i = lane; i < kNumBars; i += 32) {
+      const bool by_group = (kFp8 && i < kBarEmpty) || (i >= kBarRawEmpty && i < kBarS) || (i >= kBarP && i < kBarO) ||
+                            i == kBarMergeFree || i == kBarMergeFull;
+      mbar_init(bar(i), by_group ? 128 : 1);
     }
-    for (int s = 0; s < Shape::kRawStages; ++s) {
-      mbar_init(bar(kBarRawFull + s), 1);
-      mbar_init(bar(kBarRawEmpty + s), 128);
-    }
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(bar(kBarQ + t), 128);
-      mbar_init(bar(kBarS + t), 1);
-      mbar_init(bar(kBarP + t), 128);
-      mbar_init(bar(kBarPTail + t), 128);
-      mbar_init(bar(kBarO + t), 1);
-    }
-    mbar_init(bar(kBarMergeFree), 128);
-    mbar_init(bar(kBarMergeFull), 128);
-    for (int i = 0; i < kLoaders; ++i) mbar_init(bar(kBarTail + i), 1);
-    mbar_init(bar(kBarDrain), 1);
+    if (lane == 0) *reinterpret_cast<volatile uint32_t*>(smem + Shape::kBars + 8 * kSlotStop) = 0;
     fence_mbar_init();
-    *reinterpret_cast<volatile uint32_t*>(smem + Shape::kBars + 8 * kSlotStop) = 0;
   }
   if (warp == 9) tmem_alloc(bar(kSlotTmem), kTmemColumns);
   fence_before();
@@ -435,6 +428,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       if constexpr (kFp8) {
         if (all_steps > 0) rs *= row_factor[(solo ? 0 : t) * 128 + row];
       }
+      const bool idle = (solo ? 0 : t * kChunkTileRows) + 32 * (warp & 3) >= x.n_rows;   // a warp without a row
       // ---- the steps
       float m = -INFINITY, l = 0.f;
       bool ok = true;
@@ -443,6 +437,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         ok = wait_warp(bar(kBarS + t), j & 1, stop);
         if (!ok) break;
         fence_after();
+        if (idle) {   // its rows of P may hold anything: they reach its rows of O alone, which nobody reads
+          arrive(bar(kBarP + t));
+          arrive(bar(kBarPTail + t));
+          continue;
+        }
         float s[128];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(s + 32 * c, s_tmem + 32 * c);
@@ -541,7 +540,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           if (!wait_warp(bar(kBarMergeFull), 0, stop)) break;
         } else {
           if (!wait_warp(bar(kBarMergeFree), 0, stop)) break;
-          if (steps > 0) {
+          if (idle) {
+          } else if (steps > 0) {
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
               float o[32];
@@ -571,25 +571,31 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       const float inv = l > 0.f ? p.v_scale / l : 0.f;
       const float lse = l > 0.f ? (m * rs + lg2(l)) * 0.6931471805599453f : (l == 0.f ? -INFINITY : l);
-      const int tile_row = (solo ? 0 : t * kChunkTileRows) + row;
+      const int warp_row = (solo ? 0 : t * kChunkTileRows) + 32 * (warp & 3);
+      if (warp_row >= x.n_rows) break;   // no row of this warp's
+      const int tile_row = warp_row + lane;
       const bool valid = tile_row < x.n_rows;
+      const RowMap rows_out(p, x.row0);
       int token, head;
-      RowMap(p, x.row0).at(p, valid ? tile_row : 0, token, head);
+      rows_out.at(p, valid ? tile_row : 0, token, head);
       const int64_t out_row = (int64_t(x.q_start) + token) * p.num_q_heads + x.head * p.group + head;
       const int64_t part_row = (int64_t(x.slot) + tile_row) * p.num_kv_heads + x.head;
       if (valid) {
         if (x.slot >= 0) p.partial_lse[part_row] = lse;
         else if (p.lse != nullptr) p.lse[out_row] = lse;
       }
-      const float* const part = reinterpret_cast<const float*>(smem);
-#pragma unroll
-      for (int c = 0; c < D; c += 32) {
-        float o[32];
+      // Through shared memory, so that the warp writes whole rows: its 32 rows of 2 D bytes (the fp32 partial results in two
+      // halves) lie, 16-byte vectors permuted by row, in the Q tile that nobody reads any more (solo: the ring's).
+      constexpr int kRowBytes = 2 * D, kRowLanes = kRowBytes / 16, kHalves = 2;
+      const uint32_t out_stage = (solo ? base + Shape::kRing : q_tiles + t * Shape::kTileBytes) + uint32_t(warp & 3) * (32 * kRowBytes);
+      const uint32_t my_row = out_stage + uint32_t(lane) * kRowBytes;
+      auto result = [&](float* o, int c) {   // columns c .. c + 31 of this thread's row
         if (all_steps > 0) {
           tmem_ld32(o, o_tmem + c);
           wait_ld();
           settle<32>(o);
           if (solo) {
+            const float* const part = reinterpret_cast<const float*>(smem);
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] = o[i] * w + part[(c + i) * 128 + row] * w1;
           }
@@ -597,18 +603,54 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         // a row that has seen nothing is zero whatever the accumulator holds
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? o[i] * inv : (l == 0.f ? 0.f : l);
-        if (!valid) continue;
-        if (x.slot >= 0) {
-          float4* dst = reinterpret_cast<float4*>(p.partial_o + part_row * D + c);
+      };
+      auto write_rows = [&](auto address) {   // address(token, head, row): where the row's kRowBytes go
+        __syncwarp();
+#pragma unroll 4
+        for (int i = 0; i < kRowLanes; ++i) {
+          const int r = i * (32 / kRowLanes) + lane / kRowLanes, vec = lane % kRowLanes;
+          const int r_item = warp_row + r;
+          if (r_item < x.n_rows) {
+            int token_r, head_r;
+            rows_out.at(p, r_item, token_r, head_r);
+            reinterpret_cast<uint4*>(address(token_r, head_r, r_item))[vec] =
+                ld_shared(out_stage + uint32_t(r) * kRowBytes + uint32_t((vec ^ (r & 7)) << 4));
+          }
+        }
+        __syncwarp();
+      };
+      if (x.slot < 0) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-        } else {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + out_row * D + c);
+        for (int c = 0; c < D; c += 32) {
+          float o[32];
+          result(o, c);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            dst[i] = make_uint4(pack<true>(o[8 * i], o[8 * i + 1]), pack<true>(o[8 * i + 2], o[8 * i + 3]),
-                                pack<true>(o[8 * i + 4], o[8 * i + 5]), pack<true>(o[8 * i + 6], o[8 * i + 7]));
+            st_shared(my_row + uint32_t(((c / 8 + i) ^ (lane & 7)) << 4),
+                      make_uint4(pack<true>(o[8 * i], o[8 * i + 1]), pack<true>(o[8 * i + 2], o[8 * i + 3]),
+                                 pack<true>(o[8 * i + 4], o[8 * i + 5]), pack<true>(o[8 * i + 6], o[8 * i + 7])));
           }
+        }
+        write_rows([&](int token_r, int head_r, int) {
+          return p.out + ((int64_t(x.q_start) + token_r) * p.num_q_heads + x.head * p.group + head_r) * D;
+        });
+      } else {
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) {
+#pragma unroll
+          for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
+            float o[32];
+            result(o, c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              st_shared(my_row + uint32_t((((c - half * (D / 2)) / 4 + i) ^ (lane & 7)) << 4),
+                        make_uint4(__float_as_uint(o[4 * i]), __float_as_uint(o[4 * i + 1]), __float_as_uint(o[4 * i + 2]),
+                                   __float_as_uint(o[4 * i + 3])));
+            }
+          }
+          write_rows([&](int, int, int r_item) {
+            return p.partial_o + ((int64_t(x.slot) + r_item) * p.num_kv_heads + x.head) * D + half * (D / 2);
+          });
         }
       }
     } while (false);
@@ -882,10 +924,11 @@ constexpr int kChunkMergeWarps = 8;
 // grid = (merges x KV heads, ceil(kChunkItemRows / kChunkMergeWarps))
 template <int D>
 __global__ void __launch_bounds__(kChunkMergeWarps * 32) chunk_merge_kernel(const ChunkMergeParams p) {
-  if (__ldg(p.serial_at) != p.serial) return;   // the attention kernel has said so
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // every thread: see combine_kernel
+  if (*p.serial_at != p.serial) return;   // the attention kernel has said so
   constexpr int V = D / 32;
   const int lane = threadIdx.x & 31;
-  const int4 a = __ldg(p.merges + 2 * (blockIdx.x / p.num_kv_heads)), b = __ldg(p.merges + 2 * (blockIdx.x / p.num_kv_heads) + 1);
+  const int4 a = p.merges[2 * (blockIdx.x / p.num_kv_heads)], b = p.merges[2 * (blockIdx.x / p.num_kv_heads) + 1];
   const int head = blockIdx.x % p.num_kv_heads, n_rows = a.z, n = b.x;
   const int r = blockIdx.y * kChunkMergeWarps + (threadIdx.x >> 5);
   if (r >= n_rows) return;
