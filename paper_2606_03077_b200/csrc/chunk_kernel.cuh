@@ -542,7 +542,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           if (!wait_warp(bar(kBarMergeFree), 0, stop)) break;
           if (idle) {
           } else if (steps > 0) {
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < D; c += 32) {
               float o[32];
               tmem_ld32(o, o_tmem + c);
@@ -569,7 +569,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         l = l * w + l1 * w1;
         m = to;
       }
-      const float inv = l > 0.f ? p.v_scale / l : 0.f;
+      const float inv = p.v_scale / l;
       const float lse = l > 0.f ? (m * rs + lg2(l)) * 0.6931471805599453f : (l == 0.f ? -INFINITY : l);
       const int warp_row = (solo ? 0 : t * kChunkTileRows) + 32 * (warp & 3);
       if (warp_row >= x.n_rows) break;   // no row of this warp's
@@ -584,6 +584,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (x.slot >= 0) p.partial_lse[part_row] = lse;
         else if (p.lse != nullptr) p.lse[out_row] = lse;
       }
+      // The loops from here on are not unrolled: this code runs once a block, and in a block's first run on a multiprocessor
+      // fetching it takes longer than running it (6300 cycles unrolled, 1900 as it is).
       // Through shared memory, so that the warp writes whole rows: its 32 rows of 2 D bytes (the fp32 partial results in two
       // halves) lie, 16-byte vectors permuted by row, in the Q tile that nobody reads any more (solo: the ring's).
       constexpr int kRowBytes = 2 * D, kRowLanes = kRowBytes / 16, kHalves = 2;
@@ -602,11 +604,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         }
         // a row that has seen nothing is zero whatever the accumulator holds
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = l > 0.f ? o[i] * inv : (l == 0.f ? 0.f : l);
+        for (int i = 0; i < 32; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
       };
       auto write_rows = [&](auto address) {   // address(token, head, row): where the row's kRowBytes go
         __syncwarp();
-#pragma unroll 4
+#pragma unroll 2
         for (int i = 0; i < kRowLanes; ++i) {
           const int r = i * (32 / kRowLanes) + lane / kRowLanes, vec = lane % kRowLanes;
           const int r_item = warp_row + r;
@@ -620,7 +622,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         __syncwarp();
       };
       if (x.slot < 0) {
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           float o[32];
           result(o, c);
@@ -635,9 +637,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           return p.out + ((int64_t(x.q_start) + token_r) * p.num_q_heads + x.head * p.group + head_r) * D;
         });
       } else {
-#pragma unroll
+#pragma unroll 1
         for (int half = 0; half < kHalves; ++half) {
-#pragma unroll
+#pragma unroll 1
           for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
             float o[32];
             result(o, c);
