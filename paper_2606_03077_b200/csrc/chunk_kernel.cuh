@@ -70,9 +70,11 @@ struct ChunkShape {
   static constexpr int kRawStages = kFp8 ? (D == 128 ? 4 : 8) : 0;
   // An item with one row tile leaves the second Q tile's place free: the ring is one stage longer then, and begins there.
   static constexpr int kSoloStages = kStages < 8 ? kStages + 1 : kStages;
+  // Quarters of a step's probabilities that the product with V starts on (the other one: 1 - 2 % slower)
+  static constexpr int kPEarly = kFp8 ? 3 : 2;
   static constexpr int kThreads = kFp8 ? 512 : 384;
   // registers a thread of each role: together what the launch brings (384 x 168, 512 x 128)
-  static constexpr int kSoftmaxRegs = kFp8 ? 184 : 216, kIssueRegs = 72, kConvertRegs = 72;
+  static constexpr int kSoftmaxRegs = kFp8 ? 184 : 224, kIssueRegs = kFp8 ? 72 : 56, kConvertRegs = 72;
   static constexpr int kLaunchRegs = kFp8 ? 512 * 128 : 384 * 168;
   static_assert(256 * kSoftmaxRegs + 128 * kIssueRegs + (kFp8 ? 128 * kConvertRegs : 0) <= kLaunchRegs, "setmaxnreg would wait");
   // dynamic shared memory: Q tiles | ring | raw ring | floats | barriers
@@ -91,7 +93,6 @@ using namespace dev;
 // barriers, in 8-byte slots after the floats
 constexpr int kBarFull = 0, kBarEmpty = 8, kBarRawFull = 16, kBarRawEmpty = 24, kBarQ = 32, kBarS = 34, kBarP = 36, kBarPTail = 38,
               kBarO = 40, kBarMergeFree = 42, kBarMergeFull = 43, kBarDrain = 44, kBarTail = 45, kNumBars = 48;
-constexpr int kPEarly = 3;    // quarters of a step's probabilities that the second product starts on
 constexpr int kLoaders = 3;   // warps 8, 10 and 11 take the ring's tiles by turns
 constexpr int kSlotStop = 48, kSlotTmem = 49;   // the stop flag and the tensor-memory address live in two more slots
 
@@ -462,7 +463,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
           return max3(max3(mx[0], mx[1], s[124]), max3(mx[2], mx[3], s[125]), fmaxf(s[126], s[127]));
         };
-        if (j == 0) m = row_max();
         float2 sum[2], shift2;
         const float2 rs2 = make_float2(rs, rs);
         uint32_t pk[16];
@@ -481,7 +481,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           shift2 = make_float2(x, x);
         };
         // The first quarter goes by the running maximum as it stands, while this tile's maximum is being found: the
-        // exponentials keep their unit busy meanwhile.  It is done again where the maximum turns out to be too low.
+        // exponentials keep their unit busy meanwhile.  It is done again where the maximum turns out to be too low, as
+        // it does in the first step.
         set_shift();
         probabilities(0);
         const float tile_max = row_max();
@@ -512,7 +513,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         for (int part = 1; part < 4; ++part) {
           probabilities(part);
           tmem_st16(s_tmem + 16 * part, pk);
-          if (part == kPEarly - 1) {   // the product starts on these while the rest is being worked out
+          if (part == Shape::kPEarly - 1) {   // the product starts on these while the rest is being worked out
             wait_st();
             fence_before();
             arrive(bar(kBarP + t));
@@ -798,7 +799,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 ok = ok && wait_warp(bar(kBarP + t), (n_p >> t) & 1, stop);
                 if (!ok) break;
                 fence_after();
-                if (leader) values(t, v_low, i0 == 0, 0, 2 * kPEarly);
+                if (leader) values(t, v_low, i0 == 0, 0, 2 * Shape::kPEarly);
                 ok = wait_warp(bar(kBarPTail + t), (n_p >> t) & 1, stop);
                 n_p ^= 1u << t;
               }
@@ -806,7 +807,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
               fence_after();
               if (leader) {
                 if (now) {
-                  values(t, v_low, false, 2 * kPEarly, kChunkKvTile / 16);
+                  values(t, v_low, false, 2 * Shape::kPEarly, kChunkKvTile / 16);
                   if (t == 1) commit(bar(kBarEmpty + v_stage));
                   if (!more) commit(bar(kBarO + t));
                 }
@@ -833,13 +834,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 if (!ok) break;
                 fence_after();
                 uint32_t v_low = uniform(ring_low + kVLow + v_stage * kTileLow);
-                if (leader) values(t, v_low, i0 == 0, 0, 2 * kPEarly);
+                if (leader) values(t, v_low, i0 == 0, 0, 2 * Shape::kPEarly);
                 ok = wait_warp(bar(kBarPTail + t), (n_p >> t) & 1, stop);
                 if (!ok) break;
                 n_p ^= 1u << t;
                 fence_after();
                 v_low = uniform(ring_low + kVLow + v_stage * kTileLow);
-                if (leader) values(t, v_low, false, 2 * kPEarly, kChunkKvTile / 16);
+                if (leader) values(t, v_low, false, 2 * Shape::kPEarly, kChunkKvTile / 16);
                 signal(kBarEmpty + v_stage);
                 if (i + 2 >= turns) signal(kBarO + t);
               }
