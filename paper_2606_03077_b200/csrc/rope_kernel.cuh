@@ -19,6 +19,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "libra.h"
 
@@ -80,11 +81,6 @@ template <int V, bool kHalf>
 __host__ __device__ __forceinline__ int rotating_items(int rotary_dim) {
   return kHalf ? rotary_dim / (2 * V) : rotary_dim / V;
 }
-template <int V, bool kHalf>
-__host__ __device__ __forceinline__ int items_per_head(int rotary_dim, int head_dim) {
-  return rotating_items<V, kHalf>(rotary_dim) + (head_dim - rotary_dim) / V;
-}
-
 // A thread keeps one item j and walks over rows (token, head): no division but one multiplication per row.
 struct Walk {
   int j;      // item
@@ -141,64 +137,66 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const __grid_c
   }
   __syncthreads();
   const int rot = rope::rotating_items<V, kHalf>(p.rope.rotary_dim);
-  const int per_head = rope::items_per_head<V, kHalf>(p.rope.rotary_dim, p.head_dim);
-  const bool in_place = p.x == p.out;
-  const rope::Walk walk(per_head);
   const int rows = nt * p.n_heads;
   constexpr int kAtOnce = kVector && kHalf ? 1 : 2;   // rows whose loads are in flight together (twice as many: 5 - 8 % slower)
-  for (int j = walk.j; j < per_head; j += kRopeThreads) {
-    const bool turns = j < rot;
-    if (!turns && in_place) continue;
-    const int c = turns ? j * V : p.rope.rotary_dim + (j - rot) * V;
-    for (int r0 = walk.first; r0 < rows; r0 += kAtOnce * walk.step) {
-      alignas(16) T a[kAtOnce][V];
-      alignas(16) T b[kAtOnce][V];
-      int64_t dst[kAtOnce];
-      int tok[kAtOnce];
+  // First the items that rotate, then those that pass: together in a warp they would each wait for the other's code.
+  auto run = [&](auto is_turning, int per_head) {
+    constexpr bool turns = decltype(is_turning)::value;
+    const rope::Walk walk(per_head);
+    for (int j = walk.j; j < per_head; j += kRopeThreads) {
+      const int c = (turns ? 0 : p.rope.rotary_dim) + j * V;
+      for (int r0 = walk.first; r0 < rows; r0 += kAtOnce * walk.step) {
+        alignas(16) T a[kAtOnce][V];
+        alignas(16) T b[kAtOnce][V];
+        int64_t dst[kAtOnce];
+        int tok[kAtOnce];
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int row = r0 + u * walk.step;
-        tok[u] = -1;
-        if (row < rows) {
-          tok[u] = int(__umulhi(uint32_t(row), p.heads_inverse));
-          if (p.n_heads == 1) tok[u] = row;
-          const int head = row - tok[u] * p.n_heads;
-          const T* src = static_cast<const T*>(p.x) + (t0 + tok[u]) * p.x_stride_token + head * p.x_stride_head + c;
-          dst[u] = (t0 + tok[u]) * p.out_stride_token + head * p.out_stride_head + c;
-          rope::load<T, V, kVector>(src, a[u]);
-          if (kHalf && turns) rope::load<T, V, kVector>(src + pairs, b[u]);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        if (tok[u] < 0) continue;
-        T* to = static_cast<T*>(p.out) + dst[u];
-        if (turns) {
-          const float2* f = cs + tok[u] * pairs + j;
-          const int pitch = rot;   // pairs / (V or V / 2)
-          if constexpr (kHalf) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-              const float2 w = f[k * pitch];
-              const float x = rope::to_f32(a[u][k]), y = rope::to_f32(b[u][k]);
-              a[u][k] = rope::from_f32<T>(x * w.x - y * w.y);
-              b[u][k] = rope::from_f32<T>(x * w.y + y * w.x);
-            }
-            rope::store<T, V, kVector>(to + pairs, b[u]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < V; k += 2) {
-              const float2 w = f[(k / 2) * pitch];
-              const float x = rope::to_f32(a[u][k]), y = rope::to_f32(a[u][k + 1]);
-              a[u][k] = rope::from_f32<T>(x * w.x - y * w.y);
-              a[u][k + 1] = rope::from_f32<T>(x * w.y + y * w.x);
-            }
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int row = r0 + u * walk.step;
+          tok[u] = -1;
+          if (row < rows) {
+            tok[u] = int(__umulhi(uint32_t(row), p.heads_inverse));
+            if (p.n_heads == 1) tok[u] = row;
+            const int head = row - tok[u] * p.n_heads;
+            const T* src = static_cast<const T*>(p.x) + (t0 + tok[u]) * p.x_stride_token + head * p.x_stride_head + c;
+            dst[u] = (t0 + tok[u]) * p.out_stride_token + head * p.out_stride_head + c;
+            rope::load<T, V, kVector>(src, a[u]);
+            if (kHalf && turns) rope::load<T, V, kVector>(src + pairs, b[u]);
           }
         }
-        rope::store<T, V, kVector>(to, a[u]);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          if (tok[u] < 0) continue;
+          T* to = static_cast<T*>(p.out) + dst[u];
+          if (turns) {
+            const float2* f = cs + tok[u] * pairs + j;
+            const int pitch = rot;   // pairs / (V or V / 2)
+            if constexpr (kHalf) {
+#pragma unroll
+              for (int k = 0; k < V; ++k) {
+                const float2 w = f[k * pitch];
+                const float x = rope::to_f32(a[u][k]), y = rope::to_f32(b[u][k]);
+                a[u][k] = rope::from_f32<T>(x * w.x - y * w.y);
+                b[u][k] = rope::from_f32<T>(x * w.y + y * w.x);
+              }
+              rope::store<T, V, kVector>(to + pairs, b[u]);
+            } else {
+#pragma unroll
+              for (int k = 0; k < V; k += 2) {
+                const float2 w = f[(k / 2) * pitch];
+                const float x = rope::to_f32(a[u][k]), y = rope::to_f32(a[u][k + 1]);
+                a[u][k] = rope::from_f32<T>(x * w.x - y * w.y);
+                a[u][k + 1] = rope::from_f32<T>(x * w.y + y * w.x);
+              }
+            }
+          }
+          rope::store<T, V, kVector>(to, a[u]);
+        }
       }
     }
-  }
+  };
+  run(std::true_type(), rot);
+  if (p.x != p.out && p.head_dim > p.rope.rotary_dim) run(std::false_type(), (p.head_dim - p.rope.rotary_dim) / V);
 }
 
 struct RopeAppendParams {
@@ -298,86 +296,89 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
   }
   __syncthreads();
   const int rot = rope::rotating_items<V, kHalf>(p.rope.rotary_dim);
-  const int per_head = rope::items_per_head<V, kHalf>(p.rope.rotary_dim, p.head_dim);
   const int q_heads = p.heads - 2 * p.num_kv_heads;
-  const rope::Walk walk(per_head);
   const int rows = nt * p.heads;
   constexpr int kAtOnce = kVector ? (kHalf ? 2 : 4) : 2;   // rows whose loads are in flight together (half: 4 % slower, twice: up to 60 %)
-  for (int j = walk.j; j < per_head; j += kRopeThreads) {
-    const bool turns = j < rot;
-    const int c = turns ? j * V : p.rope.rotary_dim + (j - rot) * V;
-    for (int r0 = walk.first; r0 < rows; r0 += kAtOnce * walk.step) {
-      alignas(16) __nv_bfloat16 a[kAtOnce][V];
-      alignas(16) __nv_bfloat16 b[kAtOnce][V];
-      int tok[kAtOnce], head[kAtOnce];
+  auto run = [&](auto is_turning, int per_head) {   // items that rotate (those of values are copied), items that pass
+    constexpr bool turns = decltype(is_turning)::value;
+    const rope::Walk walk(per_head);
+    for (int j = walk.j; j < per_head; j += kRopeThreads) {
+      const int c = (turns ? 0 : p.rope.rotary_dim) + j * V;
+      for (int r0 = walk.first; r0 < rows; r0 += kAtOnce * walk.step) {
+        alignas(16) __nv_bfloat16 a[kAtOnce][V];
+        alignas(16) __nv_bfloat16 b[kAtOnce][V];
+        int tok[kAtOnce], head[kAtOnce];
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int row = r0 + u * walk.step;
-        tok[u] = -1;
-        if (row < rows) {
-          tok[u] = int(__umulhi(uint32_t(row), p.heads_inverse));
-          head[u] = row - tok[u] * p.heads;
-          const int64_t slot = s_slot[tok[u]];
-          // a row behind the last sequence; a key or value that is not stored
-          if (slot == -2 || (slot < 0 && head[u] >= q_heads)) {
-            tok[u] = -1;
-          } else {
-            const int64_t at = t0 + tok[u];
-            const __nv_bfloat16* src =
-                head[u] < q_heads ? p.q + at * p.q_stride + head[u] * p.head_dim
-                : head[u] < q_heads + p.num_kv_heads ? p.k_new + at * p.kv_stride + (head[u] - q_heads) * p.head_dim
-                                                     : p.v_new + at * p.kv_stride + (head[u] - q_heads - p.num_kv_heads) * p.head_dim;
-            rope::load<__nv_bfloat16, V, kVector>(src + c, a[u]);
-            if (kHalf && turns) rope::load<__nv_bfloat16, V, kVector>(src + c + pairs, b[u]);
-          }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        if (tok[u] < 0) continue;
-        const bool is_q = head[u] < q_heads, is_v = head[u] >= q_heads + p.num_kv_heads;
-        float x[V], y[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) x[k] = __bfloat162float(a[u][k]);
-        if (kHalf && turns) {
-#pragma unroll
-          for (int k = 0; k < V; ++k) y[k] = __bfloat162float(b[u][k]);
-        }
-        if (turns && !is_v) {
-          const float2* f = cs + tok[u] * pairs + j;
-          const int pitch = rot;   // pairs / (V or V / 2)
-          if constexpr (kHalf) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-              const float2 w = f[k * pitch];
-              const float s = x[k], t = y[k];
-              x[k] = s * w.x - t * w.y;
-              y[k] = s * w.y + t * w.x;
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < V; k += 2) {
-              const float2 w = f[(k / 2) * pitch];
-              const float s = x[k], t = x[k + 1];
-              x[k] = s * w.x - t * w.y;
-              x[k + 1] = s * w.y + t * w.x;
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int row = r0 + u * walk.step;
+          tok[u] = -1;
+          if (row < rows) {
+            tok[u] = int(__umulhi(uint32_t(row), p.heads_inverse));
+            head[u] = row - tok[u] * p.heads;
+            const int64_t slot = s_slot[tok[u]];
+            // a row behind the last sequence; a key or value that is not stored
+            if (slot == -2 || (slot < 0 && head[u] >= q_heads)) {
+              tok[u] = -1;
+            } else {
+              const int64_t at = t0 + tok[u];
+              const __nv_bfloat16* src =
+                  head[u] < q_heads ? p.q + at * p.q_stride + head[u] * p.head_dim
+                  : head[u] < q_heads + p.num_kv_heads ? p.k_new + at * p.kv_stride + (head[u] - q_heads) * p.head_dim
+                                                       : p.v_new + at * p.kv_stride + (head[u] - q_heads - p.num_kv_heads) * p.head_dim;
+              rope::load<__nv_bfloat16, V, kVector>(src + c, a[u]);
+              if (kHalf && turns) rope::load<__nv_bfloat16, V, kVector>(src + c + pairs, b[u]);
             }
           }
         }
-        if (is_q) {
-          __nv_bfloat16* to = p.q_out + int64_t(t0 + tok[u]) * p.q_out_stride + head[u] * p.head_dim + c;
-          rope::store_pool<__nv_bfloat16, V, kVector>(to, x, 1.f);
-          if (kHalf && turns) rope::store_pool<__nv_bfloat16, V, kVector>(to + pairs, y, 1.f);
-        } else {
-          const int kv_head = head[u] - q_heads - (is_v ? p.num_kv_heads : 0);
-          P* to = static_cast<P*>(is_v ? p.v_pool : p.k_pool) + s_slot[tok[u]] + kv_head * p.stride_head + c;
-          const float inv = is_v ? p.v_inv_scale : p.k_inv_scale;
-          rope::store_pool<P, V, kVector>(to, x, inv);
-          if (kHalf && turns) rope::store_pool<P, V, kVector>(to + pairs, y, inv);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          if (tok[u] < 0) continue;
+          const bool is_q = head[u] < q_heads, is_v = head[u] >= q_heads + p.num_kv_heads;
+          float x[V], y[V];
+#pragma unroll
+          for (int k = 0; k < V; ++k) x[k] = __bfloat162float(a[u][k]);
+          if (kHalf && turns) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) y[k] = __bfloat162float(b[u][k]);
+          }
+          if (turns && !is_v) {
+            const float2* f = cs + tok[u] * pairs + j;
+            const int pitch = rot;   // pairs / (V or V / 2)
+            if constexpr (kHalf) {
+#pragma unroll
+              for (int k = 0; k < V; ++k) {
+                const float2 w = f[k * pitch];
+                const float s = x[k], t = y[k];
+                x[k] = s * w.x - t * w.y;
+                y[k] = s * w.y + t * w.x;
+              }
+            } else {
+#pragma unroll
+              for (int k = 0; k < V; k += 2) {
+                const float2 w = f[(k / 2) * pitch];
+                const float s = x[k], t = x[k + 1];
+                x[k] = s * w.x - t * w.y;
+                x[k + 1] = s * w.y + t * w.x;
+              }
+            }
+          }
+          if (is_q) {
+            __nv_bfloat16* to = p.q_out + int64_t(t0 + tok[u]) * p.q_out_stride + head[u] * p.head_dim + c;
+            rope::store_pool<__nv_bfloat16, V, kVector>(to, x, 1.f);
+            if (kHalf && turns) rope::store_pool<__nv_bfloat16, V, kVector>(to + pairs, y, 1.f);
+          } else {
+            const int kv_head = head[u] - q_heads - (is_v ? p.num_kv_heads : 0);
+            P* to = static_cast<P*>(is_v ? p.v_pool : p.k_pool) + s_slot[tok[u]] + kv_head * p.stride_head + c;
+            const float inv = is_v ? p.v_inv_scale : p.k_inv_scale;
+            rope::store_pool<P, V, kVector>(to, x, inv);
+            if (kHalf && turns) rope::store_pool<P, V, kVector>(to + pairs, y, inv);
+          }
         }
       }
     }
-  }
+  };
+  if (rot > 0) run(std::true_type(), rot);
+  if (p.head_dim > p.rope.rotary_dim) run(std::false_type(), (p.head_dim - p.rope.rotary_dim) / V);
 }
 
 }  // namespace libra
