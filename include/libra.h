@@ -500,7 +500,8 @@ int libra_rope_init(libra_rope_t* rope, int32_t rotary_dim, int32_t layout, doub
 /* Rotate rows of heads: x and out are device arrays [n_tokens, n_heads, head_dim] of `dtype` on `device`, element
  * (t, h, c) at t * stride_token + h * stride_head + c; positions is int32[n_tokens] on the device.  direction
  * LIBRA_ROPE_FORWARD is the map above; LIBRA_ROPE_GRADIENT is its transpose, which takes the gradient of the output to the
- * gradient of the input (magnitude included).  out may be x (with the same strides); any other overlap is not allowed.
+ * gradient of the input (magnitude included).  out may be x (with the same strides); any other overlap is not allowed, and
+ * the rows of out do not overlap (tokens apart by all heads of one, or heads by all tokens of one).
  * Arithmetic in float32, one rounding to `dtype`.  head_dim is even, rotary_dim <= head_dim <= 1024, n_heads <= 16384; rows need no more than the
  * element's own alignment (16-byte aligned ones are faster).  Asynchronous on `stream`; nothing is allocated.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE, CUDA_ERROR. */

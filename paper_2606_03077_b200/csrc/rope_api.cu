@@ -56,8 +56,14 @@ int libra_rope_apply(int32_t device, const libra_rope_t* rope, const void* x, vo
   if (!valid_rope(rope) || dtype < LIBRA_ROPE_BF16 || dtype > LIBRA_ROPE_F32) return LIBRA_INVALID_ARGUMENT;
   if (direction != LIBRA_ROPE_FORWARD && direction != LIBRA_ROPE_GRADIENT) return LIBRA_INVALID_ARGUMENT;
   if (x_stride_token < 0 || x_stride_head < 0 || out_stride_token < 0 || out_stride_head < 0) return LIBRA_INVALID_ARGUMENT;
-  // rows of the output must not overlap one another
+  // rows of the output must not overlap one another: all heads of a token before the next token, or all tokens of a head before
+  // the next head
   if ((n_tokens > 1 && out_stride_token < head_dim) || (n_heads > 1 && out_stride_head < head_dim)) return LIBRA_INVALID_ARGUMENT;
+  if (n_tokens > 1 && n_heads > 1) {
+    const __int128 heads_span = __int128(n_heads - 1) * out_stride_head + head_dim;
+    const __int128 tokens_span = __int128(n_tokens - 1) * out_stride_token + head_dim;
+    if (out_stride_token < heads_span && out_stride_head < tokens_span) return LIBRA_INVALID_ARGUMENT;
+  }
   if (x == out && (x_stride_token != out_stride_token || x_stride_head != out_stride_head)) return LIBRA_INVALID_ARGUMENT;
   if (head_dim % 2 != 0 || head_dim > 1024 || rope->rotary_dim > head_dim) return LIBRA_UNSUPPORTED_SHAPE;
   if (n_heads > kMaxHeads || n_tokens > 0x7fffffff) return LIBRA_UNSUPPORTED_SHAPE;

@@ -105,7 +105,7 @@ class Case:
             seen = np.isfinite(w)
             assert np.array_equal(np.isneginf(g), ~seen)
             bound = np.broadcast_to((e_s + 2.0 ** -20)[..., 0] if L else 0.0, w.shape) + 2.0 ** -20 * np.abs(np.where(seen, w, 0))
-            assert np.all(np.abs(g - w)[seen] <= bound[seen]), float((np.abs(g - w)[seen] / bound[seen]).max())
+            assert np.all(np.abs(g[seen] - w[seen]) <= bound[seen]), float((np.abs(g[seen] - w[seen]) / bound[seen]).max())
             r += n
 
     def run(self):
@@ -395,6 +395,61 @@ def test_far_into_a_large_pool(lib):
     ref, _, spread = K.packed_chunk_attention(q.double().cpu().numpy(), [kt], [vt], [n], [L])
     assert np.all(np.abs(out.double().cpu().numpy() - ref) <= (2.0 ** -8 + 2.0 ** -14) * spread * 1.01 + 2.0 ** -8 * np.abs(ref))
     h.close()
+
+
+def test_sequences_that_share_pages(lib):
+    """A common beginning held once: both block tables name the same pages."""
+    c = Case(lib, [30, 7], [100, 100], 8, 2, 128, seed=18)
+    c.bt[1, :4] = c.bt[0, :4]
+    c.dbt.copy_(c.torch.from_numpy(c.bt))
+    c.run()
+
+
+def test_launches_that_are_not_dependent_give_the_same_bits(lib):
+    c = Case(lib, [40, 3], [3000, 90], 8, 2, 128, seed=19)
+    c.plan(); c.attn()
+    want = c.out.clone()
+    c.h.set_dependent_launch(False)
+    c.out.fill_(0x7FC0)
+    c.attn()
+    assert c.torch.equal(c.out, want)
+    c.check(); c.h.close()
+
+
+def test_more_items_than_a_grid_dimension_holds(lib):
+    """70,000 sequences of one token: each row of out is its value row."""
+    import torch
+    n = 70000
+    k, v, q = (torch.randn((n, 1, 16, 64), device="cuda").to(torch.bfloat16) for _ in range(3))
+    k[:, :, 1:], v[:, :, 1:] = float("nan"), float("nan")
+    h = lib.Handle(1, 1, 64, n, n, 1)
+    bt = torch.randperm(n, device="cuda").to(torch.int32)
+    ws = torch.empty(h.chunk_workspace_size(n), dtype=torch.uint8, device="cuda")
+    out, err = torch.empty((n, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    st = torch.cuda.current_stream().cuda_stream
+    h.chunk_plan(np.ones(n, np.int32), np.ones(n, np.int32), ws.data_ptr(), ws.numel(), st)
+    rows = q[:, 0, 0].contiguous()
+    h.chunk_attn(rows.data_ptr(), 64, k.data_ptr(), v.data_ptr(), bt.data_ptr(), out.data_ptr(), 0, err.data_ptr(), st)
+    assert int(err) == 0 and torch.equal(out, v[bt.long(), 0, 0])
+    h.close()
+
+
+def test_pools_of_the_other_type_after_the_plan(lib):
+    """The plan does not depend on the pools' type: one plan, attention over E4M3 pools and then over bf16 ones."""
+    c8 = Case(lib, [20, 3], [300, 90], 8, 2, 128, seed=20, kv="e4m3")
+    c16 = Case(lib, [20, 3], [300, 90], 8, 2, 128, seed=20)
+    c8.h.close()
+    c8.h = c16.h
+    assert c8.kh.shape == c16.kh.shape
+    c16.plan()
+    c8.h.set_kv_dtype(lib.KV_E4M3, *c8.scales)
+    c8.attn()
+    c8.check()
+    c16.h.set_kv_dtype(lib.KV_BF16)
+    c16.attn()
+    c16.check()
+    assert int(c8.err) == 0 and int(c16.err) == 0
+    c16.h.close()
 
 
 def test_refusals(lib):

@@ -48,7 +48,7 @@ def apply(lib, rope, x, out, positions, dtype, direction):
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("tokens,heads,dim,rotary,scaling", [
     (1, 1, 2, 2, "none"), (1, 32, 128, 128, "none"), (7, 3, 80, 80, "linear"), (37, 5, 96, 32, "base"), (130, 2, 64, 64, "bands"),
-    (3, 1, 256, 256, "ramp"), (5, 4, 66, 10, "ramp"), (1200, 1, 64, 24, "none"), (2500, 2, 8, 8, "none")])
+    (3, 1, 256, 256, "ramp"), (5, 4, 66, 10, "ramp"), (1200, 1, 64, 24, "none"), (2500, 2, 8, 8, "none"), (3, 2, 1024, 250, "none"), (700, 3, 1024, 256, "linear")])
 def test_apply(lib, tokens, heads, dim, rotary, scaling, dtype, layout, gradient):
     import torch
     rope = rope_of(lib, rotary, layout, 10000.0, scaling)
@@ -89,6 +89,24 @@ def test_apply_strided_in_place_and_unaligned(lib, layout):
         keep = torch.ones_like(wide, dtype=torch.bool)
         torch.as_strided(keep, (tokens, heads, dim), (stride, dim + gap, 1), off).fill_(False)
         assert torch.equal(wide[keep], before[keep])
+
+
+def test_apply_on_head_major_rows_and_another_stream(lib):
+    """[heads, tokens, channels], as attention over dense keys wants it, from and into; the call on a side stream."""
+    import torch
+    rng = np.random.default_rng(9)
+    tokens, heads, dim = 50, 6, 64
+    rope, pos = rope_of(lib, 64), torch.from_numpy(rng.integers(0, 5000, 50).astype(np.int32)).cuda()
+    x = torch.from_numpy(rng.standard_normal((heads, tokens, dim))).to(torch.bfloat16).cuda()
+    out = torch.full_like(x, float("nan"))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        apply(lib, rope, x.transpose(0, 1), out.transpose(0, 1), pos, "bf16", lib.ROPE_FORWARD)
+    side.synchronize()
+    xs = x.transpose(0, 1).double().cpu().numpy()
+    ref = K.rotate(xs, K.rope_angles(pos.cpu().numpy(), K.rope_turns(64, 10000.0)), K.HALF)
+    assert np.all(np.abs(out.transpose(0, 1).double().cpu().numpy() - ref) <= bound(xs, ref, 64, K.HALF, 1.0, "bf16"))
 
 
 @pytest.mark.parametrize("layout", [K.HALF, K.INTERLEAVED])

@@ -85,6 +85,8 @@ def test_refusals_of_apply_and_append_before_a_gpu_is_touched(lib):
         (dict(head_dim=1026, n_heads=1), lib.UNSUPPORTED_SHAPE), (dict(head_dim=32), lib.UNSUPPORTED_SHAPE), (dict(dtype=3), lib.INVALID_ARGUMENT),
         (dict(direction=2), lib.INVALID_ARGUMENT), (dict(x_stride_token=-128), lib.INVALID_ARGUMENT),
         (dict(n_tokens=2, out_stride_token=32), lib.INVALID_ARGUMENT), (dict(out_stride_head=32), lib.INVALID_ARGUMENT),
+        (dict(n_tokens=2, out_stride_token=64), lib.INVALID_ARGUMENT), (dict(n_tokens=3, out_stride_token=64, out_stride_head=128), lib.INVALID_ARGUMENT),
+        (dict(n_heads=16385), lib.UNSUPPORTED_SHAPE),
         (dict(x_ptr=4096, x_stride_token=256), lib.INVALID_ARGUMENT), (dict(x_ptr=257), lib.INVALID_ARGUMENT),
         (dict(x_ptr=258, dtype=lib.ROPE_F32), lib.INVALID_ARGUMENT), (dict(rope=lib.Rope()), lib.INVALID_ARGUMENT),
     ]:
