@@ -206,25 +206,16 @@ int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const vo
   if (guard.err != cudaSuccess) return fail_cuda(h, guard.err);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
 
-  libra_handle_s::PoolMaps* pm = nullptr;
-  for (auto& m : c.maps) {
-    if (m.k_ptr == k_pages && m.v_ptr == v_pages) pm = &m;
+  // whole pages: 64 channels with 128-byte swizzle as the tensor cores read them, or an 8-bit row as it is
+  const int row_bytes = h->fp8 ? h->cfg.head_dim : 128;
+  const CUtensorMapSwizzle swizzle = h->fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
+  CUtensorMap map_k, map_v;
+  int pos_head = 0, pos_page = 0, pos_token = 0;
+  int rc = libra::encode_pool_map(h, k_pages, row_bytes, h->cfg.page_size, swizzle, &map_k, &pos_head, &pos_page, &pos_token);
+  if (rc == LIBRA_OK) {
+    rc = libra::encode_pool_map(h, v_pages, row_bytes, h->cfg.page_size, swizzle, &map_v, &pos_head, &pos_page, &pos_token);
   }
-  if (!pm) {
-    pm = &c.maps[c.next_map];
-    c.next_map = (c.next_map + 1) % libra_handle_s::kMapCache;
-    pm->k_ptr = pm->v_ptr = nullptr;
-    // whole pages: 64 channels with 128-byte swizzle as the tensor cores read them, or an 8-bit row as it is
-    const int row_bytes = h->fp8 ? h->cfg.head_dim : 128;
-    const CUtensorMapSwizzle swizzle = h->fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
-    int rc = libra::encode_pool_map(h, k_pages, row_bytes, h->cfg.page_size, swizzle, &pm->map_k, &c.pos_head, &c.pos_page, &c.pos_token);
-    if (rc == LIBRA_OK) {
-      rc = libra::encode_pool_map(h, v_pages, row_bytes, h->cfg.page_size, swizzle, &pm->map_v, &c.pos_head, &c.pos_page, &c.pos_token);
-    }
-    if (rc != LIBRA_OK) return rc;
-    pm->k_ptr = k_pages;
-    pm->v_ptr = v_pages;
-  }
+  if (rc != LIBRA_OK) return rc;
 
   uint8_t* ws = static_cast<uint8_t*>(c.workspace);
   libra::ChunkParams p;
@@ -247,15 +238,15 @@ int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const vo
   p.group_inverse = uint32_t((65536 + h->group - 1) / h->group);
   p.block_table_ld = h->cfg.block_table_ld;
   p.page_shift = h->cfg.page_size == 16 ? 4 : (h->cfg.page_size == 32 ? 5 : 6);
-  p.pos_head = c.pos_head;
-  p.pos_page = c.pos_page;
-  p.pos_token = c.pos_token;
+  p.pos_head = pos_head;
+  p.pos_page = pos_page;
+  p.pos_token = pos_token;
   p.scale_log2 = h->scale_log2 * h->k_scale;
   p.v_scale = h->v_scale;
   const int di = h->cfg.head_dim == 128 ? 1 : 0;
   const ChunkBuild& b = kBuilds[di][h->fp8 ? 1 : 0];
   const dim3 blocks(unsigned(p.num_kv_heads), unsigned(std::min(c.n_items, 65535)), unsigned((c.n_items + 65534) / 65535));
-  LIBRA_CUDA_TRY(h, launch(h->pdl, b.fn, blocks, unsigned(b.threads), size_t(b.smem), st, pm->map_k, pm->map_v, p));
+  LIBRA_CUDA_TRY(h, launch(h->pdl, b.fn, blocks, unsigned(b.threads), size_t(b.smem), st, map_k, map_v, p));
   ++h->launches;
   if (c.n_merges > 0) {
     libra::ChunkMergeParams m;

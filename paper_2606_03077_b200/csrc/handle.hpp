@@ -98,16 +98,13 @@ struct libra_handle_s {
   int next_map = 0;
   int pos_head = 0, pos_page = 0, pos_token = 0;
 
-  // chunk attention: its own plan, workspace and tensor maps
+  // chunk attention: its own plan and workspace
   struct Chunk {
     bool planned = false;
     uint32_t serial = 0;              // of the plan, also in the workspace
     void* workspace = nullptr;
     int32_t n_items = 0, n_merges = 0;
     size_t merges_off = 0, lse_off = 0, o_off = 0;
-    PoolMaps maps[kMapCache];
-    int next_map = 0;
-    int pos_head = 0, pos_page = 0, pos_token = 0;
     void* staging[2] = {nullptr, nullptr};   // pinned, grown when a plan needs more
     size_t staging_bytes[2] = {0, 0};
     cudaEvent_t staging_done[2] = {nullptr, nullptr};

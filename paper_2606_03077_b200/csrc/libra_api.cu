@@ -707,10 +707,7 @@ int libra_set_kv_dtype(libra_handle_t h, int32_t dtype, float k_scale, float v_s
   h->fp8_variant = -1;
   h->k_scale = h->fp8 ? k_scale : 1.f;
   h->v_scale = h->fp8 ? v_scale : 1.f;
-  for (int i = 0; i < libra_handle_s::kMapCache; ++i) {  // maps depend on the type
-    h->maps[i].k_ptr = h->maps[i].v_ptr = nullptr;
-    h->chunk.maps[i].k_ptr = h->chunk.maps[i].v_ptr = nullptr;
-  }
+  for (int i = 0; i < libra_handle_s::kMapCache; ++i) h->maps[i].k_ptr = h->maps[i].v_ptr = nullptr;  // maps depend on the type
   return LIBRA_OK;
 }
 

@@ -13,7 +13,7 @@
 // apart) per thread and step.  V is 16 bytes' worth where pointers, strides and the rotated part allow it, else items
 // of one channel (half) or one pair (interleaved).
 //
-// Measured: 8191 x 40 heads of 128 channels, 64 rotated in neighbouring pairs, 35 us = 4.8 TB/s (74 % of a plain copy: loads in flight
+// Measured: 8191 x 40 heads of 128 channels, 64 rotated in neighbouring pairs, 33 us = 5.0 TB/s (77 % of a plain copy: loads in flight
 // and instruction issue); float32, 16384 x 16 x 64, 23.5 us = 5.7 TB/s; append of 15K ragged tokens, 40 + 16 heads, 91 us = 5.4 TB/s;
 // 16K tokens into an E4M3 cache 107 us = 5.9 TB/s.
 #pragma once
@@ -30,8 +30,8 @@
 namespace libra {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeMaxTokens = 4;   // tokens per block at most: with 8 a block is too long, with 2 the sines weigh (43.9, 41.6 and
-                                    // 45.7 us for 2, 4, 8 tokens: 8191 tokens of 40 heads, 64 of 128 channels rotated)
+constexpr int kRopeMaxTokens = 4;   // tokens per block at most: with 8 a block is too long, with 2 the sines weigh (37.2, 35.4 and
+                                    // 39.4 us for 2, 4, 8 tokens: 8191 tokens of 40 heads, 64 of 128 channels rotated)
 
 namespace rope {
 
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const __grid_c
   __syncthreads();
   const int rot = rope::rotating_items<V, kHalf>(p.rope.rotary_dim);
   const int rows = nt * p.n_heads;
-  constexpr int kAtOnce = kVector && kHalf ? 1 : 2;   // rows whose loads are in flight together (twice as many: 5 - 8 % slower)
+  constexpr int kAtOnce = kVector ? 1 : 2;   // rows whose loads are in flight together (twice as many: 5 - 8 % slower)
   // First the items that rotate, then those that pass: together in a warp they would each wait for the other's code.
   auto run = [&](auto is_turning, int per_head) {
     constexpr bool turns = decltype(is_turning)::value;
