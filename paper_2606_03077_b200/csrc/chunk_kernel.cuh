@@ -439,7 +439,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       float rs = p.scale_log2;   // score -> base-2 exponent
       if constexpr (kFp8) {
-        if (all_steps > 0) rs *= row_factor[(solo ? 0 : t) * 128 + row];
+        // The product with the factor of a row of zeros, or nearly so, may lie below the smallest normal number and be flushed to
+        // zero, and -inf * 0 is no masked score.  At that number scores of up to 2^27 weigh all tokens alike, as they should.
+        if (all_steps > 0) rs = fmaxf(rs * row_factor[(solo ? 0 : t) * 128 + row], 0x1p-126f);
       }
       const bool idle = (solo ? 0 : t * kChunkTileRows) + 32 * (warp & 3) >= x.n_rows;   // a warp without a row
       // ---- the steps
