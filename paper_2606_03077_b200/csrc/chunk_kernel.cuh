@@ -437,12 +437,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         // the row factors come from the group that loaded the tile
         if (!wait_warp(bar(kBarQ + (solo ? 0 : t)), 0, stop)) break;
       }
-      float rs = p.scale_log2;   // score -> base-2 exponent
-      if constexpr (kFp8) {
-        // The product with the factor of a row of zeros, or nearly so, may lie below the smallest normal number and be flushed to
-        // zero, and -inf * 0 is no masked score.  At that number scores of up to 2^27 weigh all tokens alike, as they should.
-        if (all_steps > 0) rs = fmaxf(rs * row_factor[(solo ? 0 : t) * 128 + row], 0x1p-126f);
-      }
+      auto row_scale = [&] {   // score -> base-2 exponent
+        if constexpr (kFp8) {
+          // The product with the factor of a row of zeros, or nearly so, may lie below the smallest normal number and be flushed to
+          // zero, and -inf * 0 is no masked score.  At that number scores of up to 2^27 weigh all tokens alike, as they should.
+          if (all_steps > 0) return fmaxf(p.scale_log2 * row_factor[(solo ? 0 : t) * 128 + row], 0x1p-126f);
+        }
+        return p.scale_log2;
+      };
+      float rs = row_scale();
       const bool idle = (solo ? 0 : t * kChunkTileRows) + 32 * (warp & 3) >= x.n_rows;   // a warp without a row
       // ---- the steps
       float m = -INFINITY, l = 0.f;
@@ -477,8 +480,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
           return max3(max3(mx[0], mx[1], s[124]), max3(mx[2], mx[3], s[125]), fmaxf(s[126], s[127]));
         };
-        float2 sum[2], shift2;
-        const float2 rs2 = make_float2(rs, rs);
+        float2 sum[2], shift2, rs2;
         uint32_t pk[16];
         auto probabilities = [&](int part) {   // of 32 columns
 #pragma unroll
@@ -493,6 +495,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         auto set_shift = [&] {
           const float x = m == -INFINITY ? 0.f : -m * rs;
           shift2 = make_float2(x, x);
+          rs2 = make_float2(rs, rs);
         };
         // The first quarter goes by the running maximum as it stands, while this tile's maximum is being found: the
         // exponentials keep their unit busy meanwhile.  It is done again where the maximum turns out to be too low, as
@@ -506,6 +509,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           const float alpha = to == -INFINITY ? 1.f : ex2((m - to) * rs);
           m = to;
           l *= alpha;
+          // Rounding m * rs multiplies all of the row's probabilities by a power of two whose exponent is the rounding error.  Below
+          // 2^24 that is at most a half, and cancels in the result; beyond, it could exceed what a float32 holds.  Scores are whole
+          // units apart there: a power of two takes the place of rs, and the product is exact.
+          if (m != -INFINITY && fabsf(m * rs) >= 0x1p24f) rs = __uint_as_float(__float_as_uint(rs) & 0x7f800000u);
           if (j > 0) {
 #pragma unroll
             for (int c = 0; c < D; c += 16) {
@@ -542,6 +549,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       if (!ok) break;
       // ---- the result.  Of the item only what the steps need was kept; it is read again while the last product ends.
       x = load_unit(p);
+      rs = row_scale();
       if (all_steps > 0) {
         if (!wait_warp(bar(kBarO + t), 0, stop)) break;
         fence_after();
