@@ -976,10 +976,10 @@ __global__ void __launch_bounds__(kChunkMergeWarps * 32) chunk_merge_kernel(cons
 #pragma unroll
     for (int v = 0; v < V; ++v) num[v] += w * src[int64_t(i) * pitch * D + v];
   }
-  const float inv = den > 0.f ? 1.f / den : 0.f;
+  const float inv = den == 0.f ? 0.f : 1.f / den;   // 0: a row that sees nothing; NaN stays NaN
   const int flat = a.y + r, token = flat / p.group;
   const int64_t row = (int64_t(a.x) + token) * p.num_q_heads + head * p.group + flat - token * p.group;
-  if (p.lse != nullptr && lane == 0) p.lse[row] = den > 0.f ? m + __logf(den) : -INFINITY;
+  if (p.lse != nullptr && lane == 0) p.lse[row] = den == 0.f ? -INFINITY : m + __logf(den);
 #pragma unroll
   for (int v = 0; v < V; v += 2) {
     *reinterpret_cast<__nv_bfloat162*>(p.out + row * D + lane * V + v) = __floats2bfloat162_rn(num[v] * inv, num[v + 1] * inv);
