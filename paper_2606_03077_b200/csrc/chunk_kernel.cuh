@@ -36,7 +36,8 @@
 // power of two that brings its largest element to 2^10 .. 2^11: elements 2^-25 below it and larger stay exact, the rest lose
 // less than a float32 product would.  P is rounded to fp16.
 //
-// Every wait is bounded; the first one that runs out sets the block's stop flag and the error word, and every role leaves.
+// Every wait is bounded; the first one that runs out sets the block's stop flag and the error word, and every role leaves.  Once all
+// have, the copies and products under way are waited for (bounded), before the block's memory goes to another.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -46,6 +47,7 @@
 #include <cstdint>
 
 #include "chunk_plan.hpp"
+#include "chunk_ring.hpp"
 #include "libra.h"
 #include "ptx.cuh"
 
@@ -105,7 +107,8 @@ using namespace dev;
 // barriers, in 8-byte slots after the floats
 constexpr int kBarFull = 0, kBarEmpty = 8, kBarRawFull = 16, kBarRawEmpty = 24, kBarQ = 32, kBarS = 34, kBarP = 36, kBarPTail = 38,
               kBarO = 40, kBarMergeFree = 42, kBarMergeFull = 43, kBarDrain = 44, kBarTail = 45, kNumBars = 48;
-constexpr int kLoaders = 3;   // warps 8, 10 and 11 take the ring's tiles by turns
+constexpr int kLoaders = kChunkLoaders;   // warps 8, 10 and 11
+constexpr int kDrainTries = 4096;   // of the waits that end a block early, some 2 us each
 constexpr int kSlotStop = 48, kSlotTmem = 49;   // the stop flag and the tensor-memory address live in two more slots
 
 struct Stop {   // how a wait that ran out ends the block
@@ -384,6 +387,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   const bool solo = load_unit(p).solo;
   const int n_stages = solo ? Shape::kSoloStages : Shape::kStages;
   const uint32_t ring = base + Shape::kRing - uint32_t(n_stages - Shape::kStages) * Shape::kTileBytes;
+  int next_copy = -1;         // a copying warp's next tile when it left; -1: it has asked for none
+  bool tail_copy = false;     // its newest one signals kBarTail and not the tile's own barrier
 
   if (run && warp < 8) {
     // ------------------------------------------------------------------ softmax group t: row tile t (both: tile 0 if solo)
@@ -693,7 +698,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       const int my_page = lane & ((1 << tile_pages_shift) - 1), my_box = lane >> tile_pages_shift;
       const int page_tokens = 1 << p.page_shift;
       const ChunkUnit x = load_unit(p);
-      uint32_t n_tail = 0, phase = 0;
+      uint32_t phase = 0;
       int i = loader, stage = loader;   // the next tile that this warp brings, and its place (a ring has three stages or more)
       bool ok = true;
       if (i < 2 * x.steps) {
@@ -733,10 +738,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 "l"(reinterpret_cast<uint64_t>(is_v ? &map_v : &map_k)), "r"(signal), "r"(my_box * 64), "r"(c1), "r"(c2), "r"(c3)
                 : "memory");
           }
-          if (tail) {   // rows behind the range are zeroed before the tile is handed on
-            ok = wait_warp(signal, n_tail & 1, stop);
-            if (!ok) break;
-            ++n_tail;
+          if (tail) {   // rows behind the range are zeroed before the tile is handed on; a block has one such tile, its last
+            ok = wait_warp(signal, 0, stop);
+            if (!ok) {
+              tail_copy = true;
+              i += kLoaders;
+              break;
+            }
             const int chunks = (kChunkKvTile - left) * (D / 8);
             for (int k = lane; k < chunks; k += 32) {
               st_shared(dst + swizzled(left + k / (D / 8), k % (D / 8)), make_uint4(0, 0, 0, 0));
@@ -752,11 +760,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
         }
       }
-      if (!ok) {   // leave no copy in flight behind: wait (bounded) for this warp's last fills
-        for (int g = i - kLoaders; g >= 0 && g >= i - n; g -= kLoaders) {
-          for (int k = 0; k < 4096 && !mbar_try_wait(bar(kFull + g % n), (g / n) & 1); ++k) {}
-        }
-      }
+      next_copy = i;
     } else if (run && warp == 9) {
       // ------------------------------------------------------------------ tensor-core instructions
       // The whole warp walks through the steps and one lane issues: what the instructions take (descriptors, addresses) is then
@@ -879,10 +883,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         }
         if (ok && turns == 1 && leader) commit(bar(kBarO + 1));   // group 1 has no turn
       }
-      if (!ok) {   // nothing may be in flight when the tensor memory is given back
-        if (leader) commit(bar(kBarDrain));
-        for (uint32_t i = 0; i < 4096 && !mbar_try_wait(bar(kBarDrain), 0); ++i) {}
-      }
     }
   } else if (kFp8 && warp >= 12) {
     if constexpr (kFp8) {
@@ -929,6 +929,21 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   fence_before();
   __syncthreads();
   fence_after();
+  if (stop.set()) {   // a wait has run out, and no role starts anything more: what is under way ends before the block does
+    if (warp == 9) {   // the products
+      if (elect_one()) commit(bar(kBarDrain));   // the lane that issued them: the same one is elected every time
+      for (int k = 0; k < kDrainTries && !mbar_try_wait(bar(kBarDrain), 0); ++k) {}
+      __syncwarp();
+    } else if (next_copy >= 0) {   // this warp's copies
+      const int n = kFp8 ? Shape::kRawStages : n_stages;
+      constexpr int kFull = kFp8 ? kBarRawFull : kBarFull;
+      for (int g = ring_newest(next_copy); ring_may_fly(g, next_copy, n); g = ring_before(g)) {
+        const bool tail = tail_copy && g == ring_newest(next_copy);
+        const uint32_t b = tail ? bar(kBarTail + (warp == 8 ? 0 : warp - 9)) : bar(kFull + g % n), parity = tail ? 0 : (g / n) & 1;
+        for (int k = 0; k < kDrainTries && !mbar_try_wait(b, parity); ++k) {}
+      }
+    }
+  }
   if (warp == 9) tmem_dealloc(tmem, kTmemColumns);
 }
 
