@@ -575,7 +575,7 @@ int libra_chunk_plan(libra_handle_t handle, const int32_t* q_lens_host, const in
  * The launch may be recorded in a CUDA graph: a replay uses the plan in the workspace, which therefore has to stay (if another
  * plan was put there the replay computes nothing and says so in the error word), and the partial results in it, so two
  * graphs whose replays can overlap need a workspace each.  Asynchronous on `stream`.
- * Errors: INVALID_ARGUMENT, NOT_PLANNED, CUDA_ERROR. */
+ * Errors: INVALID_ARGUMENT (also: sm_scale * k_scale * log2(e), or v_scale, is no normal float32), NOT_PLANNED, CUDA_ERROR. */
 int libra_chunk_attn(libra_handle_t handle, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
                      const int32_t* block_table, void* out, float* lse, void* error_word_dev, void* stream);
 

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 
@@ -199,6 +200,8 @@ int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const vo
   if (off(q, 16) || off(k_pages, 16) || off(v_pages, 16) || off(out, 16) || off(block_table, 4) || off(lse, 4) || off(error_word_dev, 4)) {
     return LIBRA_INVALID_ARGUMENT;
   }
+  // the kernels flush what is not normal to zero
+  if (!std::isnormal(h->scale_log2 * h->k_scale) || !std::isnormal(h->v_scale)) return LIBRA_INVALID_ARGUMENT;
   libra_handle_s::Chunk& c = h->chunk;
   if (!c.planned) return LIBRA_NOT_PLANNED;
   if (c.n_items == 0) return LIBRA_OK;
