@@ -530,7 +530,8 @@ int libra_rope_apply(int32_t device, const libra_rope_t* rope, const void* x, vo
  * multiples of 8; no two rows of a call may name the same slot.  Bits of *error_word_dev (32-bit device word):
  * LIBRA_ERR_BAD_PAGE_ID for a page id outside the pool, LIBRA_ERR_PLAN_OVERFLOW for a token past the end of a block-table
  * row; such a token is not stored.  The handle supplies the pool geometry and type; no plan, no workspace.  Asynchronous on
- * `stream`.  Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (rotary_dim > head_dim; more than 16384 heads together), CUDA_ERROR. */
+ * `stream`.  Errors: INVALID_ARGUMENT (also: E4M3 pools and 1 / k_scale or 1 / v_scale is no normal float32), UNSUPPORTED_SHAPE
+ * (rotary_dim > head_dim; more than 16384 heads together), CUDA_ERROR. */
 int libra_rope_append(libra_handle_t handle, const libra_rope_t* rope, const void* q, int64_t q_stride, void* q_out,
                       int64_t q_out_stride, const void* k_new, const void* v_new, int64_t kv_stride,
                       const int32_t* q_offsets, const int32_t* seq_lens, const int32_t* block_table, int32_t batch,

@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "handle.hpp"
@@ -126,6 +127,8 @@ int libra_rope_append(libra_handle_t h, const libra_rope_t* rope, const void* q,
       !aligned(error_word_dev, 4)) {
     return LIBRA_INVALID_ARGUMENT;
   }
+  // the kernel flushes what is not normal to zero
+  if (h->fp8 && (!std::isnormal(1.f / h->k_scale) || !std::isnormal(1.f / h->v_scale))) return LIBRA_INVALID_ARGUMENT;
   if (rope && rope->rotary_dim > D) return LIBRA_UNSUPPORTED_SHAPE;
   const int heads = (q ? h->cfg.num_q_heads : 0) + 2 * h->cfg.num_kv_heads;
   if (heads > kMaxHeads) return LIBRA_UNSUPPORTED_SHAPE;
