@@ -48,6 +48,22 @@ __device__ __forceinline__ float2 cos_sin(int32_t pos, uint64_t turns, float mag
   return make_float2(cr * magnitude, sr * magnitude);
 }
 
+// (x, y) turned by the angle whose cosine and sine are w, in instructions that keep numbers below the smallest normal one (the
+// build's default flushes them to zero, and a bf16 or float32 value may be one).
+__device__ __forceinline__ float mul_rn(float a, float b) {
+  float d;
+  asm("mul.rn.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float fma_rn(float a, float b, float c) {
+  float d;
+  asm("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float2 turned(float x, float y, float2 w) {
+  return make_float2(fma_rn(x, w.x, mul_rn(y, -w.y)), fma_rn(x, w.y, mul_rn(y, w.x)));
+}
+
 template <typename T> __device__ __forceinline__ float to_f32(T x);
 template <> __device__ __forceinline__ float to_f32(float x) { return x; }
 template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -179,18 +195,18 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const __grid_c
 #pragma unroll
               for (int k = 0; k < V; ++k) {
                 const float2 w = f[k * pitch];
-                const float x = rope::to_f32(a[u][k]), y = rope::to_f32(b[u][k]);
-                a[u][k] = rope::from_f32<T>(x * w.x - y * w.y);
-                b[u][k] = rope::from_f32<T>(x * w.y + y * w.x);
+                const float2 z = rope::turned(rope::to_f32(a[u][k]), rope::to_f32(b[u][k]), w);
+                a[u][k] = rope::from_f32<T>(z.x);
+                b[u][k] = rope::from_f32<T>(z.y);
               }
               rope::store<T, V, kVector>(to + pairs, b[u]);
             } else {
 #pragma unroll
               for (int k = 0; k < V; k += 2) {
                 const float2 w = f[(k / 2) * pitch];
-                const float x = rope::to_f32(a[u][k]), y = rope::to_f32(a[u][k + 1]);
-                a[u][k] = rope::from_f32<T>(x * w.x - y * w.y);
-                a[u][k + 1] = rope::from_f32<T>(x * w.y + y * w.x);
+                const float2 z = rope::turned(rope::to_f32(a[u][k]), rope::to_f32(a[u][k + 1]), w);
+                a[u][k] = rope::from_f32<T>(z.x);
+                a[u][k + 1] = rope::from_f32<T>(z.y);
               }
             }
           }
@@ -352,17 +368,17 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
 #pragma unroll
               for (int k = 0; k < V; ++k) {
                 const float2 w = f[k * pitch];
-                const float s = x[k], t = y[k];
-                x[k] = s * w.x - t * w.y;
-                y[k] = s * w.y + t * w.x;
+                const float2 z = rope::turned(x[k], y[k], w);
+                x[k] = z.x;
+                y[k] = z.y;
               }
             } else {
 #pragma unroll
               for (int k = 0; k < V; k += 2) {
                 const float2 w = f[(k / 2) * pitch];
-                const float s = x[k], t = x[k + 1];
-                x[k] = s * w.x - t * w.y;
-                x[k + 1] = s * w.y + t * w.x;
+                const float2 z = rope::turned(x[k], x[k + 1], w);
+                x[k] = z.x;
+                x[k + 1] = z.y;
               }
             }
           }
