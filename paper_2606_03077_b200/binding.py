@@ -286,9 +286,16 @@ def libra_rope_apply(device: int, rope: Rope, x_ptr: int, out_ptr: int, dtype: i
            "libra_rope_apply")
 
 
+def _lengths_of_a_batch(q_lens, seq_lens):
+    ql, sl = np.asarray(q_lens, dtype=np.int32), np.asarray(seq_lens, dtype=np.int32)
+    if ql.ndim != 1 or ql.shape != sl.shape:
+        raise ValueError("q_lens and seq_lens are the lengths of one batch")
+    return _as_i32(ql), _as_i32(sl)
+
+
 def libra_chunk_plan_host(n_sm: int, num_q_heads: int, num_kv_heads: int, q_lens, seq_lens) -> dict:
     """Plan of the chunk attention as NumPy arrays: items [n, 8], merges [m, 8], and the number of partial rows."""
-    ql, sl = _as_i32(q_lens), _as_i32(seq_lens)
+    ql, sl = _lengths_of_a_batch(q_lens, seq_lens)
     n, m, rows = C.c_int32(0), C.c_int32(0), C.c_int64(0)
     p = lambda a: a.ctypes.data_as(_i32p)
     call = lambda items, merges: lib.libra_chunk_plan_host(n_sm, num_q_heads, num_kv_heads, p(ql), p(sl), len(ql), p(items),
@@ -546,9 +553,7 @@ class Handle:
 
     def chunk_plan(self, q_lens_host: np.ndarray, seq_lens_host: np.ndarray, workspace_ptr: int, workspace_bytes: int,
                    stream: int) -> None:
-        ql, sl = _as_i32(q_lens_host), _as_i32(seq_lens_host)
-        if ql.shape != sl.shape:
-            raise ValueError("q_lens and seq_lens are of one batch")
+        ql, sl = _lengths_of_a_batch(q_lens_host, seq_lens_host)
         _check(lib.libra_chunk_plan(self._h, ql.ctypes.data_as(_i32p), sl.ctypes.data_as(_i32p), int(ql.shape[0]), workspace_ptr,
                                     workspace_bytes, stream), "libra_chunk_plan")
 
