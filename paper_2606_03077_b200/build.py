@@ -77,6 +77,8 @@ def build_library(force: bool = False, verbose: bool = True, extra_flags=()) -> 
             if f.read().strip() == digest:
                 return LIB_PATH
     os.makedirs(OBJ_DIR, exist_ok=True)
+    if os.path.exists(STAMP_PATH):   # as for the objects below
+        os.remove(STAMP_PATH)
 
     def run(cmd):
         if verbose:
@@ -90,6 +92,8 @@ def build_library(force: bool = False, verbose: bool = True, extra_flags=()) -> 
             with open(stamp) as f:
                 if f.read().strip() == own:
                     return obj, None
+        if os.path.exists(stamp):   # it vouches for the object that is about to be overwritten
+            os.remove(stamp)
         res = run([_nvcc(), *NVCC_FLAGS, *extra_flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", obj])
         if res.returncode == 0:
             with open(stamp, "w") as f:
