@@ -7,6 +7,7 @@ library loads on machines without a driver (the planner entry point needs no GPU
 from __future__ import annotations
 
 import concurrent.futures
+import contextlib
 import hashlib
 import os
 import re
@@ -77,7 +78,7 @@ def build_library(force: bool = False, verbose: bool = True, extra_flags=()) -> 
             if f.read().strip() == digest:
                 return LIB_PATH
     os.makedirs(OBJ_DIR, exist_ok=True)
-    if os.path.exists(STAMP_PATH):   # as for the objects below
+    with contextlib.suppress(FileNotFoundError):   # as for the objects below
         os.remove(STAMP_PATH)
 
     def run(cmd):
@@ -92,7 +93,7 @@ def build_library(force: bool = False, verbose: bool = True, extra_flags=()) -> 
             with open(stamp) as f:
                 if f.read().strip() == own:
                     return obj, None
-        if os.path.exists(stamp):   # it vouches for the object that is about to be overwritten
+        with contextlib.suppress(FileNotFoundError):   # it vouches for the object that is about to be overwritten
             os.remove(stamp)
         res = run([_nvcc(), *NVCC_FLAGS, *extra_flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", obj])
         if res.returncode == 0:
