@@ -543,8 +543,8 @@ int libra_rope_append(libra_handle_t handle, const libra_rope_t* rope, const voi
  *   {b, first row of sequence b in q, first flattened row, rows, kv_begin, kv_end, seq_len - q_len, slot}
  * slot < 0: the range is whole.  merges: 8 int32 per cut tile: {first row of the sequence, first flattened row, rows, slot
  * of its first chunk, chunks, 0, 0, 0}; chunk j's partial rows begin at slot + j * rows; *partial_rows counts them.
- * Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (more than 2^31 - 1 rows), WORKSPACE_TOO_SMALL (a capacity, in items, is too
- * small; *num_items and *num_merges hold what is needed). */
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (more than 2^31 - 1 rows, a sequence of more than 2^31 - 512 tokens),
+ * WORKSPACE_TOO_SMALL (a capacity, in items, is too small; *num_items and *num_merges hold what is needed). */
 int libra_chunk_plan_host(int32_t n_sm, int32_t num_q_heads, int32_t num_kv_heads, const int32_t* q_lens,
                           const int32_t* seq_lens, int32_t batch, int32_t* items, int32_t items_capacity,
                           int32_t* num_items, int32_t* merges, int32_t merges_capacity, int32_t* num_merges,

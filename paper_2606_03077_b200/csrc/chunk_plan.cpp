@@ -79,7 +79,7 @@ bool make_chunk_plan(int n_sm, int num_q_heads, int num_kv_heads, const int32_t*
   std::vector<Tile> tiles;
   int64_t q_start = 0;
   for (int32_t b = 0; b < batch; ++b) {
-    if (q_lens[b] < 0 || seq_lens[b] < 0) return false;
+    if (q_lens[b] < 0 || seq_lens[b] < 0 || seq_lens[b] > kChunkMaxLen) return false;
     const int64_t rows = int64_t(q_lens[b]) * group;
     if (rows > 0x7fffffff || q_start + q_lens[b] > 0x7fffffff) return false;
     const int64_t ctx = int64_t(seq_lens[b]) - q_lens[b];

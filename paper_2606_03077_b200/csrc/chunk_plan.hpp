@@ -11,6 +11,8 @@ constexpr int kChunkTileRows = 128;                  // rows of one score tile (
 constexpr int kChunkItemRows = 2 * kChunkTileRows;   // rows of one item
 constexpr int kChunkKvTile = 128;                    // cached tokens of one step
 constexpr int kChunkMaxSplits = 64;                  // chunks of one item's KV range at most
+// A sequence's cached tokens at most: the kernel's 32-bit token numbers run up to two steps past the end.
+constexpr int32_t kChunkMaxLen = 0x7fffffff - 4 * kChunkKvTile + 1;
 
 struct ChunkItem {   // one block's work, for one KV head: 32 bytes, read as two 16-byte vectors
   int32_t b;         // row of the block table
@@ -41,7 +43,7 @@ inline int64_t chunk_max_partial_rows(int n_sm) { return int64_t(2) * n_sm * kCh
 // Items of any plan for up to max_tokens new tokens of up to max_batch sequences.
 int64_t chunk_max_items(int n_sm, int group, int64_t max_tokens, int64_t max_batch);
 
-// false: a negative length, or more rows than 32 bits count.
+// false: a negative length, one beyond kChunkMaxLen, or more rows than 32 bits count.
 bool make_chunk_plan(int n_sm, int num_q_heads, int num_kv_heads, const int32_t* q_lens, const int32_t* seq_lens, int32_t batch,
                      ChunkPlan* plan);
 
