@@ -467,7 +467,8 @@ int libra_kv_scatter(libra_handle_t handle, const void* k_dense, const void* v_d
  *   RAMP    pair(n) = R ln(original_len / (2 pi n)) / (2 ln base);  lo = max(floor(pair(high)), 0),
  *           hi = min(ceil(pair(low)), R - 1);  gone = clamp((i - lo) / max(hi - lo, 0.001), 0, 1);
  *           theta_i * (1 - gone) + theta_i / factor * gone
- * magnitude 0 = the default: 0.1 ln(factor) + 1 for RAMP, else 1.  low, high, original_len are read by BANDS and RAMP only.
+ * magnitude is kept as a (normal) float32; 0 = the default: 0.1 ln(factor) + 1 for RAMP, else 1.  low, high, original_len are read
+ * by BANDS and RAMP only.
  *
  * libra_rope_t is plain host data (copy it freely); libra_rope_init fills it and needs no GPU.  The angles are held in
  * turns as 0.64 fixed-point numbers: pos * theta is then exact modulo one turn for every 32-bit position, negative

@@ -66,6 +66,7 @@ extern "C" int libra_rope_init(libra_rope_t* rope, int32_t rotary_dim, int32_t l
   r.layout = layout;
   r.magnitude = float(s.magnitude > 0.0 ? s.magnitude
                                         : (s.kind == LIBRA_ROPE_SCALE_RAMP ? 0.1 * std::log(s.factor) + 1.0 : 1.0));
+  if (!std::isnormal(r.magnitude)) return LIBRA_INVALID_ARGUMENT;   // beyond float32, or flushed to zero by the kernels
   for (int i = 0; i < rotary_dim / 2; ++i) {
     const long double theta =
         scaled_angle(std::pow(b, -2.0L * i / rotary_dim), i, rotary_dim, static_cast<long double>(base), s);
