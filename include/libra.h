@@ -540,7 +540,8 @@ int libra_rope_append(libra_handle_t handle, const libra_rope_t* rope, const voi
 
 /* Plan of the chunk attention, a pure host function (needs no GPU).  A chunk's query rows are flattened per KV head (row
  * r = query token r / G, head r % G of the group) and cut into tiles of 256 rows; where that gives too few blocks to fill
- * n_sm multiprocessors, the KV ranges are cut too, into equal runs of 128-token steps.  items: 8 int32 each, longest first:
+ * n_sm multiprocessors, the KV ranges are cut too, into equal runs of 128-token steps; from 4 n_sm blocks (items x KV heads) on
+ * none is, however much longer one sequence is than the rest.  items: 8 int32 each, longest first:
  *   {b, first row of sequence b in q, first flattened row, rows, kv_begin, kv_end, seq_len - q_len, slot}
  * slot < 0: the range is whole.  merges: 8 int32 per cut tile: {first row of the sequence, first flattened row, rows, slot
  * of its first chunk, chunks, 0, 0, 0}; chunk j's partial rows begin at slot + j * rows; *partial_rows counts them.
@@ -556,7 +557,9 @@ int libra_chunk_plan_host(int32_t n_sm, int32_t num_q_heads, int32_t num_kv_head
 int libra_chunk_workspace_size(libra_handle_t handle, int64_t max_tokens, size_t* bytes);
 
 /* Plan a batch for libra_chunk_attn from host lengths (int32[batch] each) and enqueue the plan's copy into the workspace on
- * `stream`.  One plan serves any number of libra_chunk_attn calls on the same lengths (the layers of a model).  Independent of
+ * `stream`.  One plan serves any number of libra_chunk_attn calls on the same lengths (the layers of a model), one after another:
+ * on one stream, or on streams that events put in order, the plan's first, since cut ranges leave their partial results in the
+ * workspace.  The call takes 12 us of the host, and up to 115 us where it tries cuts (up to 26 simulated launches).  Independent of
  * libra_plan: a handle holds one plan of each kind.  Not while `stream` is being recorded (INVALID_ARGUMENT): the copy's source is
  * a buffer of the handle.  Errors: INVALID_ARGUMENT (also: a length that a block-table row cannot describe),
  * UNSUPPORTED_SHAPE, WORKSPACE_TOO_SMALL, CUDA_ERROR. */
@@ -569,9 +572,14 @@ int libra_chunk_plan(libra_handle_t handle, const int32_t* q_lens_host, const in
  * (seq_len_b - q_len_b + i < 0) gets zeros.  q: bf16, row r at r * q_stride elements (>= num_q_heads * head_dim, a multiple
  * of 8), 16-byte aligned; out: bf16 [rows, num_q_heads, head_dim], 16-byte aligned, not overlapping q; lse: float32 [rows,
  * num_q_heads] or NULL, natural logarithm, -inf for a row that sees nothing.  The K and V of all tokens, the new ones
- * included, are already in the pages.  Slots past a sequence's end and unowned pages never influence a result; a value that is
- * not finite in a slot that a sequence owns may reach every new row of that sequence and KV head, earlier ones too.
- * Probabilities are rounded to 16 bits for the tensor cores (bf16; fp16 over E4M3 pools), everything else is float32.
+ * included, are already in the pages.  Slots past a sequence's end and unowned pages never influence a result.  In a slot that a
+ * sequence owns, a K that is not finite reaches the rows that see it (out and lse are NaN where a score is), a V that is not finite
+ * may reach every new row of that sequence and KV head, in its channel, earlier rows too.
+ * Probabilities are rounded to 16 bits for the tensor cores: one bf16 number each (libra_decode_attn_multi hands over two), fp16
+ * over E4M3 pools.  There q is rounded to fp16 as well, each row scaled by a power of two: elements of 2^-25 of the row's largest
+ * and more stay exact, smaller ones are off by 2^-35 of it at most.  Everything else is float32, in which results below the
+ * smallest normal number may be flushed to zero.  Where a row's largest score (times log2(e)) is 2^24 or more in size, and scores
+ * are whole units apart, the differences between them may count for as little as half.
  * Results are bit-reproducible run to run.  Bits of *error_word_dev: LIBRA_ERR_BAD_PAGE_ID (such a page reads as zeros),
  * LIBRA_ERR_WAIT_TIMEOUT, LIBRA_ERR_PLAN_CHANGED.
  * The launch may be recorded in a CUDA graph: a replay uses the plan in the workspace, which therefore has to stay (if another

@@ -25,7 +25,8 @@
 // cycle) and as many of shared memory (128 bytes a cycle for Q, K and V operands and the copies).  4096 new tokens on 12288,
 // 64 / 8 heads: 1.44 ms = 1333 TFLOP/s in short runs, 80 % of a plain bf16 matrix product's burst rate (1663); the products and
 // copies alone take 1.17 ms, without the exponentials it is 1.39.  In runs of a tenth of a second and more the power cap holds the
-// clock at 1.62 GHz: 1.65 ms.  Three tokens on eight trajectories of 32K: 165 us = 6.4 TB/s of the cache.  Over an E4M3 cache the
+// clock at 1.62 GHz: 1.66 ms = 1160 TFLOP/s.  Three tokens on eight trajectories of 32K: 187 us = 5.7 TB/s of the cache (165 us
+// when the same inputs are read again).  Over an E4M3 cache the
 // conversion adds 96 KB of shared-memory traffic a step: 10 - 15 % slower than bf16 where arithmetic bounds.
 //
 // Copies: one tiled TMA load per page (16, 32 or 64 tokens) and 64 channels, 128-byte swizzle, into a ring of tiles.  Pages
@@ -33,8 +34,8 @@
 // past a row's limit are set to -inf by selection.
 //
 // E4M3 cache: the codes arrive as bytes and are converted to fp16 (exact).  q goes to fp16 too, every row multiplied by a
-// power of two that brings its largest element to 2^10 .. 2^11: elements 2^-25 below it and larger stay exact, the rest lose
-// less than a float32 product would.  P is rounded to fp16.
+// power of two that brings its largest element to 2^10 .. 2^11: elements 2^-25 below it and larger stay exact, the rest are off
+// by at most 2^-35 of it.  P is rounded to fp16.
 //
 // Every wait is bounded; the first one that runs out sets the block's stop flag and the error word, and every role leaves.  Once all
 // have, the copies and products under way are waited for (bounded), before the block's memory goes to another.

@@ -14,8 +14,9 @@
 // of one channel (half) or one pair (interleaved).
 //
 // Measured: 8191 x 40 heads of 128 channels, 64 rotated in neighbouring pairs, 33 us = 5.0 TB/s (77 % of a plain copy: loads in flight
-// and instruction issue); float32, 16384 x 16 x 64, 23.5 us = 5.7 TB/s; append of 15K ragged tokens, 40 + 16 heads, 91 us = 5.4 TB/s;
-// 16K tokens into an E4M3 cache 107 us = 5.9 TB/s.
+// and instruction issue); float32, 16384 x 16 x 64, 25.6 us = 5.2 TB/s; append of 15K ragged tokens, 40 + 16 heads, 92 us = 5.3 TB/s;
+// 16K tokens into an E4M3 cache 112 us = 5.6 TB/s.  Each on changing inputs.  Items of one channel or pair, which rotated parts
+// that 16 bytes do not divide fall back to, have not been timed.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
