@@ -2,8 +2,6 @@
 import numpy as np
 import pytest
 
-from paper_2606_03077_b200 import workloads as W
-
 from test_gpu_chunk import Case
 
 pytestmark = pytest.mark.gpu
