@@ -73,6 +73,11 @@ typedef enum {
 #define LIBRA_ERR_PLAN_CHANGED 16u  /* chunk attention: the workspace no longer holds the plan that the launch was made
                                        for (a recorded launch replayed after another plan); nothing was computed     */
 
+#define LIBRA_ERR_NO_PAGES 32u      /* libra_cache_extend: fewer free pages than the new tokens need; nothing was changed */
+#define LIBRA_ERR_BAD_LENGTH 64u    /* a length, a number of tokens or pages that cannot be: negative, more kept than there
+                                       are, more free pages than the pool has; nothing was changed                     */
+#define LIBRA_ERR_BAD_TREE 128u     /* a parent that does not stand before its child, kept tokens that do not ascend    */
+
 /* Planner constants (Section 4.3 of the paper: degrees are powers of two, work sorted by length,
  * min-max objective).  A zero field takes its default. */
 typedef struct {
@@ -588,6 +593,139 @@ int libra_chunk_plan(libra_handle_t handle, const int32_t* q_lens_host, const in
  * Errors: INVALID_ARGUMENT (also: sm_scale * k_scale * log2(e), or v_scale, is no normal float32), NOT_PLANNED, CUDA_ERROR. */
 int libra_chunk_attn(libra_handle_t handle, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
                      const int32_t* block_table, void* out, float* lse, void* error_word_dev, void* stream);
+
+/* ---- Pages and slots handed out on the GPU ---------------------------------------------------------------------------
+ * The bookkeeping of the paged cache for a step whose lengths the host does not see or that is recorded in a graph: the free
+ * pages are a stack in device memory, free_pages[0 .. *free_count), int32[num_pages], filled by the caller once with the
+ * pages that no sequence owns.  Pages have one owner each.  Both calls need no plan and no workspace, take at most 4096 sequences
+ * and launch one kernel; integers, the same result every time.  All pointers are device pointers; seq_lens, block_table, free_pages
+ * and free_count change in place and must not overlap one another or an input.  If a check on the device fails, error bits are set
+ * in *error_word_dev (32-bit device word) and NOTHING is changed, except that libra_cache_extend's q_offsets become all zero, so
+ * that the calls that follow find no new rows:
+ *   LIBRA_ERR_BAD_LENGTH     a negative length or number of tokens, more kept than there are, *free_count outside [0, num_pages],
+ *                            more pages going back than the pool has room for
+ *   LIBRA_ERR_PLAN_OVERFLOW  a length past the end of a block-table row (or past 2^31 - 1), more than max_rows new rows
+ *   LIBRA_ERR_NO_PAGES       more pages needed than there are
+ * Page ids are handed on as they are; the calls that use them check them.
+ *
+ * libra_cache_extend: sequence b, of seq_lens[b] tokens, gets new_tokens[b] more (0 allowed).  The pages it needs for them are taken
+ * from the top of the stack - the k-th of the batch, in the order of the sequences and of their pages, is
+ * free_pages[*free_count - 1 - k] - and written into its row of the block table.  Then, with the lengths before the call,
+ *   q_offsets[b]   int32[batch + 1]: sum of new_tokens over the sequences before b (the packed rows of the calls below)
+ *   positions[r]   int32[max_rows] or NULL: seq_lens[b] + i for row r = q_offsets[b] + i
+ *   slots[r]       int32[max_rows] or NULL: page * page_size + position % page_size, page = block_table[b][position / page_size]
+ * and seq_lens[b] grows by new_tokens[b].  Rows behind q_offsets[batch] are left as they were.
+ *
+ * libra_cache_trim: sequence b keeps its first keep_lens[b] tokens (0: it has ended); seq_lens[b] becomes that, and the pages from
+ * ceil(keep_lens[b] / page_size) on go back on the stack, in such an order that trimming what one extend has added leaves the stack
+ * as it was.  The entries of the block table stay; they are past the last page.
+ *
+ * Asynchronous on `stream`; may be recorded.  Errors: INVALID_ARGUMENT (also: new_tokens or keep_lens the same array as seq_lens),
+ * UNSUPPORTED_SHAPE (batch > 4096; num_pages * page_size > 2^31 - 1), CUDA_ERROR. */
+int libra_cache_extend(libra_handle_t handle, const int32_t* new_tokens, int32_t* seq_lens, int32_t* block_table, int32_t batch,
+                       int32_t* free_pages, int32_t* free_count, int32_t* q_offsets, int32_t* positions, int32_t* slots,
+                       int32_t max_rows, void* error_word_dev, void* stream);
+int libra_cache_trim(libra_handle_t handle, const int32_t* keep_lens, int32_t* seq_lens, int32_t* block_table, int32_t batch,
+                     int32_t* free_pages, int32_t* free_count, void* error_word_dev, void* stream);
+
+/* ---- Norms of the heads of q and k, with the rotation in the same pass --------------------------------------------------
+ * For each head x of each token (head_dim channels), with one weight per channel shared by all heads of q (of k):
+ *     r = 1 / sqrt(mean(x^2) + eps),   y = rotation(w * x * r)      (rotary positions as above; rope NULL: none)
+ * and, for the gradient dy of y,   g = transposed rotation(dy),   dx = r * (w * g - x * r * mean(w * g * x * r)),
+ *     dw = sum over tokens and heads of g * x * r.
+ * Arithmetic in float32, one rounding to the type; dw is float32.  x^2 is summed in float32: its mean must be finite there, and
+ * where it is below the smallest normal number it counts as zero.  eps is a positive, normal float32.
+ *
+ * libra_norm_rows_t describes q or k as device arrays [n_tokens, n_heads, head_dim] of `dtype` (LIBRA_ROPE_BF16 ...), element (t, h,
+ * c) at t * stride_token + h * stride_head + c; weight: [head_dim] of `dtype`.  out may be x (with the same strides); any other
+ * overlap is not allowed, and the rows of out do not overlap (tokens apart by all heads of one, or heads by all tokens of one).
+ * k NULL: q alone.  positions: int32[n_tokens] on the device (NULL allowed without rope).  head_dim is even, rotary_dim <= head_dim <=
+ * 1024, n_heads <= 16384; rows need no more than the element's own alignment (16-byte aligned ones are faster).  Asynchronous on
+ * `stream`; nothing is allocated; may be recorded.  Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE, CUDA_ERROR. */
+typedef struct {
+  const void* x;
+  void* out;
+  const void* weight;
+  int64_t x_stride_token, x_stride_head, out_stride_token, out_stride_head;   /* in elements */
+  int32_t n_heads;
+  int32_t reserved;
+} libra_norm_rows_t;
+int libra_norm_rope_apply(int32_t device, const libra_rope_t* rope, const libra_norm_rows_t* q, const libra_norm_rows_t* k,
+                          int32_t dtype, const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps, void* stream);
+
+/* The gradient of libra_norm_rope_apply from its inputs (x, weight) and the gradient of its output.  grad_x [n_tokens, n_heads,
+ * head_dim] of `dtype` may be grad_out or x (with the same strides); grad_weight: float32[head_dim], overwritten (zero for no tokens).
+ * workspace_dev: libra_norm_rope_workspace_size bytes on the device, 16-byte aligned, for the sums of the blocks; calls that can
+ * overlap need one each, replays of recorded calls too.  grad_weight is summed in a fixed order: the same bits every time.
+ * Errors: as above, WORKSPACE_TOO_SMALL. */
+typedef struct {
+  const void* x;
+  const void* grad_out;
+  const void* weight;
+  void* grad_x;
+  float* grad_weight;
+  int64_t x_stride_token, x_stride_head, grad_out_stride_token, grad_out_stride_head, grad_x_stride_token, grad_x_stride_head;
+  int32_t n_heads;
+  int32_t reserved;
+} libra_norm_grads_t;
+int libra_norm_rope_workspace_size(int32_t device, int32_t head_dim, size_t* bytes);
+int libra_norm_rope_gradient(int32_t device, const libra_rope_t* rope, const libra_norm_grads_t* q, const libra_norm_grads_t* k,
+                             int32_t dtype, const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps,
+                             void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Norm, rotation and append in one pass: libra_rope_append for rows whose positions and slots are given one by one, as
+ * libra_cache_extend and libra_tree_mask write them (a drafted token's position goes by its depth in the tree, its slot by its place),
+ * with the norms above where q_weight / k_weight (bf16[head_dim], 16-byte aligned) are not NULL.
+ *   q, q_out, k_new, v_new and their strides: as libra_rope_append; v is copied
+ *   positions     int32[max_rows] (NULL allowed without rope)
+ *   slots         int32[max_rows]: page * page_size + place in the page; -1: the row's k and v are not stored
+ *   n_rows        device word with the number of rows, e.g. &q_offsets[batch], or NULL: max_rows of them.  Rows behind it are
+ *                 left as they were
+ * No two rows of a call may name the same slot.  A slot outside the pool sets LIBRA_ERR_BAD_PAGE_ID and is not stored.  E4M3 pools
+ * as in libra_rope_append.  The handle supplies the pool geometry and type; no plan, no workspace.  Asynchronous on `stream`; may be
+ * recorded.  Errors: as libra_rope_append; UNSUPPORTED_SHAPE also for num_pages * page_size > 2^31 - 1. */
+int libra_norm_rope_append(libra_handle_t handle, const libra_rope_t* rope, const void* q_weight, const void* k_weight, float eps,
+                           const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new,
+                           int64_t kv_stride, const int32_t* positions, const int32_t* slots, const int32_t* n_rows, int32_t max_rows,
+                           void* k_pages, void* v_pages, void* error_word_dev, void* stream);
+
+/* ---- Trees of drafted tokens ------------------------------------------------------------------------------------------
+ * A step that verifies drafted tokens appends them all to the cache behind a sequence's n_cached = seq_len - n tokens, a parent
+ * before its children, and attends with every token to the cached ones, to its ancestors and to itself:
+ *   libra_cache_extend -> libra_tree_mask -> (each layer: libra_norm_rope_append, libra_tree_attn) -> the caller accepts a path
+ *   -> (each layer: libra_tree_keep) -> libra_cache_trim
+ * The new tokens are packed as above (q_offsets; seq_lens counts them).
+ *
+ * libra_tree_mask: parents[r], for row r = q_offsets[b] + i, is the place (0 .. i - 1) of the token's parent among its sequence's new
+ * ones, or -1: it follows the last cached token.  Bit j % 32 of word mask[r * mask_ld + j / 32] is set where j = i or j is an
+ * ancestor of i; all mask_ld words of a row are written.  positions[r] (or NULL) = n_cached + the number of ancestors.  A parent
+ * that does not stand before its child sets LIBRA_ERR_BAD_TREE and counts as -1; a sequence with more than 32 * mask_ld new tokens,
+ * or with rows past max_rows, sets LIBRA_ERR_PLAN_OVERFLOW, offsets that descend or are negative LIBRA_ERR_BAD_LENGTH, and its rows
+ * are left as they were.  Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (mask_ld > LIBRA_TREE_MAX_TOKENS / 32), CUDA_ERROR. */
+#define LIBRA_TREE_MAX_TOKENS 1024
+int libra_tree_mask(libra_handle_t handle, const int32_t* parents, const int32_t* q_offsets, const int32_t* seq_lens, int32_t batch,
+                    int32_t max_rows, uint32_t* mask, int32_t mask_ld, int32_t* positions, void* error_word_dev, void* stream);
+
+/* libra_chunk_attn for trees: row r = q_offsets[b] + i sees cached tokens 0 .. n_cached - 1, and new token j <= i where its row of
+ * the mask has bit j set (bits past i are ignored, and i itself is seen only where its bit is set).  A row that sees nothing gets
+ * zeros and lse -inf.  The plan is libra_chunk_plan's for the same lengths; mask: uint32[rows, mask_ld], 4-byte aligned, mask_ld * 32 >=
+ * the most new tokens of a sequence (INVALID_ARGUMENT otherwise; here mask_ld has no upper limit).  Everything else as
+ * libra_chunk_attn, with one difference: a V that is not finite in a slot that a row does not see may reach that row. */
+int libra_tree_attn(libra_handle_t handle, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
+                    const int32_t* block_table, const uint32_t* mask, int32_t mask_ld, void* out, float* lse, void* error_word_dev,
+                    void* stream);
+
+/* After the verification: kept[b * kept_ld + i], i < n_kept[b], are the places of the accepted tokens among sequence b's new ones, in
+ * ascending order (a path's are).  Their rows of K and V move to the slots n_cached + i, in the pools given (one layer's); other slots
+ * stay.  new_lens[b] (or NULL; not the same array as seq_lens) = n_cached + n_kept[b], which is what libra_cache_trim takes.  Rows that
+ * do not ascend, or more of them than there are new tokens or than kept_ld, set LIBRA_ERR_BAD_TREE, a length that cannot be
+ * LIBRA_ERR_BAD_LENGTH, one past the end of a block-table row LIBRA_ERR_PLAN_OVERFLOW: then nothing of that sequence moves and
+ * new_lens[b] = seq_lens[b].  A page id outside the pool sets LIBRA_ERR_BAD_PAGE_ID and the row is not moved.
+ * Both calls are asynchronous on `stream` and may be recorded; no plan, no workspace.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE (more 16-byte columns than a grid has blocks), CUDA_ERROR. */
+int libra_tree_keep(libra_handle_t handle, const int32_t* kept, int32_t kept_ld, const int32_t* n_kept, const int32_t* q_offsets,
+                    const int32_t* seq_lens, const int32_t* block_table, int32_t batch, void* k_pages, void* v_pages,
+                    int32_t* new_lens, void* error_word_dev, void* stream);
 
 /* ---- the paper's rollout-side schedulers, host code only (no GPU) ------------------------------------ */
 

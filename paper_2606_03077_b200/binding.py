@@ -23,6 +23,8 @@ OK, INVALID_ARGUMENT, UNSUPPORTED_SHAPE, WORKSPACE_TOO_SMALL, NOT_PLANNED, CUDA_
 KV_BF16, KV_E4M3 = 0, 1
 RING_F32, RING_BF16 = 0, 1
 ERR_WAIT_TIMEOUT, ERR_BAD_PAGE_ID, ERR_SEQ_LEN_MISMATCH, ERR_PLAN_OVERFLOW, ERR_PLAN_CHANGED = 1, 2, 4, 8, 16
+ERR_NO_PAGES, ERR_BAD_LENGTH, ERR_BAD_TREE = 32, 64, 128
+TREE_MAX_TOKENS = 1024
 
 
 class PlanParams(C.Structure):
@@ -78,6 +80,32 @@ class Rope(C.Structure):
     """libra_rope_t: the angles per position of every pair of channels (host data)."""
     _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float), ("reserved", C.c_int32),
                 ("turns", C.c_uint64 * ROPE_MAX_PAIRS)]
+
+
+class NormRows(C.Structure):
+    """libra_norm_rows_t: q or k for libra_norm_rope_apply (device pointers, strides in elements)."""
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("weight", C.c_void_p), ("x_stride_token", C.c_int64),
+                ("x_stride_head", C.c_int64), ("out_stride_token", C.c_int64), ("out_stride_head", C.c_int64),
+                ("n_heads", C.c_int32), ("reserved", C.c_int32)]
+
+    @classmethod
+    def of(cls, x, weight, out) -> "NormRows":
+        """From arrays [tokens, heads, head_dim] that know their address and strides, as tensors do."""
+        return cls(x.data_ptr(), out.data_ptr(), weight.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1),
+                   x.shape[1], 0)
+
+
+class NormGrads(C.Structure):
+    """libra_norm_grads_t: q or k for libra_norm_rope_gradient (device pointers, strides in elements)."""
+    _fields_ = [("x", C.c_void_p), ("grad_out", C.c_void_p), ("weight", C.c_void_p), ("grad_x", C.c_void_p),
+                ("grad_weight", C.c_void_p), ("x_stride_token", C.c_int64), ("x_stride_head", C.c_int64),
+                ("grad_out_stride_token", C.c_int64), ("grad_out_stride_head", C.c_int64), ("grad_x_stride_token", C.c_int64),
+                ("grad_x_stride_head", C.c_int64), ("n_heads", C.c_int32), ("reserved", C.c_int32)]
+
+    @classmethod
+    def of(cls, x, grad_out, weight, grad_x, grad_weight) -> "NormGrads":
+        return cls(x.data_ptr(), grad_out.data_ptr(), weight.data_ptr(), grad_x.data_ptr(), grad_weight.data_ptr(), x.stride(0),
+                   x.stride(1), grad_out.stride(0), grad_out.stride(1), grad_x.stride(0), grad_x.stride(1), x.shape[1], 0)
 
 
 _i32p = C.POINTER(C.c_int32)
@@ -146,6 +174,18 @@ SIGNATURES = {
     "libra_chunk_workspace_size": (C.c_int, [_vp, C.c_int64, C.POINTER(C.c_size_t)]),
     "libra_chunk_plan": (C.c_int, [_vp, _i32p, _i32p, C.c_int32, _vp, C.c_size_t, _vp]),
     "libra_chunk_attn": (C.c_int, [_vp, _vp, C.c_int64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "libra_cache_extend": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp, _vp, _vp, C.c_int32, _vp, _vp]),
+    "libra_cache_trim": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp, _vp]),
+    "libra_norm_rope_apply": (C.c_int, [C.c_int32, C.POINTER(Rope), C.POINTER(NormRows), C.POINTER(NormRows), C.c_int32, _vp,
+                                        C.c_int64, C.c_int32, C.c_float, _vp]),
+    "libra_norm_rope_workspace_size": (C.c_int, [C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]),
+    "libra_norm_rope_gradient": (C.c_int, [C.c_int32, C.POINTER(Rope), C.POINTER(NormGrads), C.POINTER(NormGrads), C.c_int32, _vp,
+                                           C.c_int64, C.c_int32, C.c_float, _vp, C.c_size_t, _vp]),
+    "libra_norm_rope_append": (C.c_int, [_vp, C.POINTER(Rope), _vp, _vp, C.c_float, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp,
+                                         C.c_int64, _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp, _vp]),
+    "libra_tree_mask": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int32, C.c_int32, _vp, C.c_int32, _vp, _vp, _vp]),
+    "libra_tree_attn": (C.c_int, [_vp, _vp, C.c_int64, _vp, _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp, _vp]),
+    "libra_tree_keep": (C.c_int, [_vp, _vp, C.c_int32, _vp, _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp, _vp, _vp]),
     "libra_rollout_dp": (C.c_int, [C.c_int32, _i32p, C.c_int32, _i32p, C.c_int32, C.POINTER(C.c_double),
                                    C.POINTER(C.c_double), _i32p, _i32p, _i32p, C.c_int32, _i32p]),
     "libra_trie_create": (C.c_int, [C.POINTER(_vp), _i32p, C.c_int32]),
@@ -307,6 +347,27 @@ def libra_chunk_plan_host(n_sm: int, num_q_heads: int, num_kv_heads: int, q_lens
         st = call(items, merges)
     _check(st, "libra_chunk_plan_host")
     return {"items": items, "merges": merges, "partial_rows": rows.value}
+
+
+def libra_norm_rope_apply(device: int, rope: Rope | None, q: NormRows, k: NormRows | None, dtype: int, positions_ptr: int,
+                          n_tokens: int, head_dim: int, eps: float, stream: int) -> None:
+    """Norm of every head of q and k (k None: of q alone) and rotation by position (rope None: none)."""
+    _check(lib.libra_norm_rope_apply(device, rope, q, k, dtype, positions_ptr or None, n_tokens, head_dim, eps, stream),
+           "libra_norm_rope_apply")
+
+
+def libra_norm_rope_workspace_size(device: int, head_dim: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib.libra_norm_rope_workspace_size(device, head_dim, C.byref(n)), "libra_norm_rope_workspace_size")
+    return n.value
+
+
+def libra_norm_rope_gradient(device: int, rope: Rope | None, q: NormGrads, k: NormGrads | None, dtype: int, positions_ptr: int,
+                             n_tokens: int, head_dim: int, eps: float, workspace_ptr: int, workspace_bytes: int,
+                             stream: int) -> None:
+    """Gradients of q, k and both weights from the gradient of libra_norm_rope_apply's output."""
+    _check(lib.libra_norm_rope_gradient(device, rope, q, k, dtype, positions_ptr or None, n_tokens, head_dim, eps, workspace_ptr,
+                                        workspace_bytes, stream), "libra_norm_rope_gradient")
 
 
 def libra_rollout_dp(n_gpus: int, lengths, tp_set, cost_coef):
@@ -562,6 +623,49 @@ class Handle:
         """Causal attention of the planned chunks of new tokens over the pages (lse_ptr 0: not wanted)."""
         _check(lib.libra_chunk_attn(self._h, q_ptr, q_stride, k_ptr, v_ptr, block_table_ptr, out_ptr, lse_ptr or None,
                                     error_word_ptr, stream), "libra_chunk_attn")
+
+    # ---- pages and slots, norm + rotation + append, trees of drafted tokens
+    def cache_extend(self, new_tokens_ptr: int, seq_lens_ptr: int, block_table_ptr: int, batch: int, free_pages_ptr: int,
+                     free_count_ptr: int, q_offsets_ptr: int, positions_ptr: int, slots_ptr: int, max_rows: int, error_word_ptr: int,
+                     stream: int) -> None:
+        """Pages, row offsets, positions and slots of new tokens (positions_ptr, slots_ptr 0: not wanted); seq_lens grow."""
+        _check(lib.libra_cache_extend(self._h, new_tokens_ptr, seq_lens_ptr, block_table_ptr, batch, free_pages_ptr, free_count_ptr,
+                                      q_offsets_ptr, positions_ptr or None, slots_ptr or None, max_rows, error_word_ptr, stream),
+               "libra_cache_extend")
+
+    def cache_trim(self, keep_lens_ptr: int, seq_lens_ptr: int, block_table_ptr: int, batch: int, free_pages_ptr: int,
+                   free_count_ptr: int, error_word_ptr: int, stream: int) -> None:
+        """seq_lens shrink to keep_lens; the pages behind go back."""
+        _check(lib.libra_cache_trim(self._h, keep_lens_ptr, seq_lens_ptr, block_table_ptr, batch, free_pages_ptr, free_count_ptr,
+                                    error_word_ptr, stream), "libra_cache_trim")
+
+    def norm_rope_append(self, rope: Rope | None, q_weight_ptr: int, k_weight_ptr: int, eps: float, q_ptr: int, q_stride: int,
+                         q_out_ptr: int, q_out_stride: int, k_new_ptr: int, v_new_ptr: int, kv_stride: int, positions_ptr: int,
+                         slots_ptr: int, n_rows_ptr: int, max_rows: int, k_ptr: int, v_ptr: int, error_word_ptr: int,
+                         stream: int) -> None:
+        """Norm (weight 0: none) and rotation of new q and k rows and append of k and v by slots (n_rows_ptr 0: max_rows rows)."""
+        _check(lib.libra_norm_rope_append(self._h, rope, q_weight_ptr or None, k_weight_ptr or None, eps, q_ptr or None, q_stride,
+                                          q_out_ptr or None, q_out_stride, k_new_ptr, v_new_ptr, kv_stride, positions_ptr or None,
+                                          slots_ptr, n_rows_ptr or None, max_rows, k_ptr, v_ptr, error_word_ptr, stream),
+               "libra_norm_rope_append")
+
+    def tree_mask(self, parents_ptr: int, q_offsets_ptr: int, seq_lens_ptr: int, batch: int, max_rows: int, mask_ptr: int,
+                  mask_ld: int, positions_ptr: int, error_word_ptr: int, stream: int) -> None:
+        """Ancestors of every drafted token as bits, and its position by depth (positions_ptr 0: not wanted)."""
+        _check(lib.libra_tree_mask(self._h, parents_ptr, q_offsets_ptr, seq_lens_ptr, batch, max_rows, mask_ptr, mask_ld,
+                                   positions_ptr or None, error_word_ptr, stream), "libra_tree_mask")
+
+    def tree_attn(self, q_ptr: int, q_stride: int, k_ptr: int, v_ptr: int, block_table_ptr: int, mask_ptr: int, mask_ld: int,
+                  out_ptr: int, lse_ptr: int, error_word_ptr: int, stream: int) -> None:
+        """chunk_attn for trees of drafted tokens, on the plan of chunk_plan."""
+        _check(lib.libra_tree_attn(self._h, q_ptr, q_stride, k_ptr, v_ptr, block_table_ptr, mask_ptr, mask_ld, out_ptr,
+                                   lse_ptr or None, error_word_ptr, stream), "libra_tree_attn")
+
+    def tree_keep(self, kept_ptr: int, kept_ld: int, n_kept_ptr: int, q_offsets_ptr: int, seq_lens_ptr: int, block_table_ptr: int,
+                  batch: int, k_ptr: int, v_ptr: int, new_lens_ptr: int, error_word_ptr: int, stream: int) -> None:
+        """Rows of the accepted tokens moved together (new_lens_ptr 0: not wanted)."""
+        _check(lib.libra_tree_keep(self._h, kept_ptr, kept_ld, n_kept_ptr, q_offsets_ptr, seq_lens_ptr, block_table_ptr, batch,
+                                   k_ptr, v_ptr, new_lens_ptr or None, error_word_ptr, stream), "libra_tree_keep")
 
     def debug_wait_selftest(self, stream: int) -> None:
         _check(lib.libra_debug_wait_selftest(self._h, stream), "libra_debug_wait_selftest")

@@ -21,8 +21,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "liblibra.so")
 STAMP_PATH = os.path.join(HERE, "liblibra.so.stamp")
 
-SOURCES = ["libra_api.cu", "rope_api.cu", "chunk_api.cu", "planner.cpp", "sched.cpp", "ring_sched.cpp",
-           "rope.cpp", "chunk_plan.cpp"]
+SOURCES = ["libra_api.cu", "rope_api.cu", "chunk_api.cu", "norm_api.cu", "table_api.cu", "tree_api.cu",
+           "planner.cpp", "sched.cpp", "ring_sched.cpp", "rope.cpp", "chunk_plan.cpp"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "--use_fast_math", "-Xcompiler", "-fPIC",

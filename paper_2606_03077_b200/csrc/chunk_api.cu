@@ -11,6 +11,7 @@
 #include "chunk_kernel.cuh"
 #include "chunk_plan.hpp"
 #include "handle.hpp"
+#include "launch.hpp"
 #include "libra.h"
 
 namespace {
@@ -25,12 +26,16 @@ struct ChunkBuild {
   int threads, smem;
   int registers;   // that the roles' setmaxnreg counts on
 };
-template <int D, bool kFp8>
+template <int D, bool kFp8, bool kTree>
 ChunkBuild build_of() {
   using S = libra::ChunkShape<D, kFp8>;
-  return {libra::chunk_kernel<D, kFp8>, S::kThreads, S::kDynamicBytes, S::kLaunchRegs};
+  return {libra::chunk_kernel<D, kFp8, kTree>, S::kThreads, S::kDynamicBytes, S::kLaunchRegs};
 }
-const ChunkBuild kBuilds[2][2] = {{build_of<64, false>(), build_of<64, true>()}, {build_of<128, false>(), build_of<128, true>()}};
+// by head_dim and pool type: chains, then trees
+const ChunkBuild kBuilds[4][2] = {{build_of<64, false, false>(), build_of<64, true, false>()},
+                                  {build_of<128, false, false>(), build_of<128, true, false>()},
+                                  {build_of<64, false, true>(), build_of<64, true, true>()},
+                                  {build_of<128, false, true>(), build_of<128, true, true>()}};
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 constexpr size_t kHeaderBytes = 256;   // the plan's serial number
@@ -41,22 +46,6 @@ uint32_t next_serial() {
   uint32_t n = ++counter;
   while (n == 0) n = ++counter;
   return n;
-}
-
-// As a programmatic dependent of its predecessor where the handle allows it; the kernels wait for that one inside.
-template <typename... P, typename... A>
-cudaError_t launch(bool dependent, void (*fn)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const A&... args) {
-  cudaLaunchConfig_t lc = {};
-  lc.gridDim = grid;
-  lc.blockDim = dim3(threads);
-  lc.dynamicSmemBytes = smem;
-  lc.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  lc.attrs = attr;
-  lc.numAttrs = dependent ? 1 : 0;
-  return cudaLaunchKernelEx(&lc, fn, args...);
 }
 
 int set_attributes(libra_handle_t h) {
@@ -71,6 +60,89 @@ int set_attributes(libra_handle_t h) {
     }
   }
   h->chunk.attributes_set = true;
+  return LIBRA_OK;
+}
+
+// Both attentions; mask null: a chain.
+int attend(libra_handle_t h, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages, const int32_t* block_table,
+           const uint32_t* mask, int32_t mask_ld, void* out, float* lse, void* error_word_dev, void* stream) {
+  if (!h || !q || !k_pages || !v_pages || !block_table || !out || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
+  if (q_stride < int64_t(h->cfg.num_q_heads) * h->cfg.head_dim || q_stride % 8 != 0) return LIBRA_INVALID_ARGUMENT;
+  auto off = [](const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; };
+  if (off(q, 16) || off(k_pages, 16) || off(v_pages, 16) || off(out, 16) || off(block_table, 4) || off(lse, 4) || off(error_word_dev, 4)) {
+    return LIBRA_INVALID_ARGUMENT;
+  }
+  // the kernels flush what is not normal to zero
+  if (!std::isnormal(h->scale_log2 * h->k_scale) || !std::isnormal(h->v_scale)) return LIBRA_INVALID_ARGUMENT;
+  libra_handle_s::Chunk& c = h->chunk;
+  if (!c.planned) return LIBRA_NOT_PLANNED;
+  if (mask && int64_t(mask_ld) * 32 < c.most_new) return LIBRA_INVALID_ARGUMENT;
+  if (c.n_items == 0) return LIBRA_OK;
+  DeviceGuard guard(h->cfg.device);
+  if (guard.err != cudaSuccess) return fail_cuda(h, guard.err);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+
+  // whole pages: 64 channels with 128-byte swizzle as the tensor cores read them, or an 8-bit row as it is
+  const int row_bytes = h->fp8 ? h->cfg.head_dim : 128;
+  const CUtensorMapSwizzle swizzle = h->fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
+  CUtensorMap map_k, map_v;
+  int pos_head = 0, pos_page = 0, pos_token = 0;
+  int rc = libra::encode_pool_map(h, k_pages, row_bytes, h->cfg.page_size, swizzle, &map_k, &pos_head, &pos_page, &pos_token);
+  if (rc == LIBRA_OK) {
+    rc = libra::encode_pool_map(h, v_pages, row_bytes, h->cfg.page_size, swizzle, &map_v, &pos_head, &pos_page, &pos_token);
+  }
+  if (rc != LIBRA_OK) return rc;
+
+  uint8_t* ws = static_cast<uint8_t*>(c.workspace);
+  libra::ChunkParams p;
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.q_stride = q_stride;
+  p.block_table = block_table;
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.lse = lse;
+  p.serial_at = reinterpret_cast<const uint32_t*>(ws);
+  p.items = reinterpret_cast<const int4*>(ws + kHeaderBytes);
+  p.partial_o = reinterpret_cast<float*>(ws + c.o_off);
+  p.partial_lse = reinterpret_cast<float*>(ws + c.lse_off);
+  p.error_word = static_cast<uint32_t*>(error_word_dev);
+  p.num_pages = h->cfg.num_pages;
+  p.serial = c.serial;
+  p.num_items = c.n_items;
+  p.num_q_heads = h->cfg.num_q_heads;
+  p.num_kv_heads = h->cfg.num_kv_heads;
+  p.group = h->group;
+  p.group_inverse = uint32_t((65536 + h->group - 1) / h->group);
+  p.block_table_ld = h->cfg.block_table_ld;
+  p.page_shift = h->cfg.page_size == 16 ? 4 : (h->cfg.page_size == 32 ? 5 : 6);
+  p.pos_head = pos_head;
+  p.pos_page = pos_page;
+  p.pos_token = pos_token;
+  p.scale_log2 = h->scale_log2 * h->k_scale;
+  p.v_scale = h->v_scale;
+  p.mask = mask;
+  p.mask_ld = mask_ld;
+  const int di = h->cfg.head_dim == 128 ? 1 : 0;
+  const ChunkBuild& b = kBuilds[di + (mask ? 2 : 0)][h->fp8 ? 1 : 0];
+  const dim3 blocks(unsigned(p.num_kv_heads), unsigned(std::min(c.n_items, 65535)), unsigned((c.n_items + 65534) / 65535));
+  LIBRA_CUDA_TRY(h, libra::launch(h->pdl, 1, b.fn, blocks, unsigned(b.threads), size_t(b.smem), st, map_k, map_v, p));
+  ++h->launches;
+  if (c.n_merges > 0) {
+    libra::ChunkMergeParams m;
+    m.merges = reinterpret_cast<const int4*>(ws + c.merges_off);
+    m.serial_at = p.serial_at;
+    m.partial_o = p.partial_o;
+    m.partial_lse = p.partial_lse;
+    m.out = p.out;
+    m.lse = lse;
+    m.serial = c.serial;
+    m.num_q_heads = p.num_q_heads;
+    m.num_kv_heads = p.num_kv_heads;
+    m.group = p.group;
+    const dim3 grid(unsigned(c.n_merges * p.num_kv_heads), unsigned(libra::kChunkItemRows / libra::kChunkMergeWarps));
+    LIBRA_CUDA_TRY(h, libra::launch(h->pdl, 1, di ? libra::chunk_merge_kernel<128> : libra::chunk_merge_kernel<64>, grid,
+                             unsigned(libra::kChunkMergeWarps * 32), 0, st, m));
+    ++h->launches;
+  }
   return LIBRA_OK;
 }
 
@@ -183,6 +255,8 @@ int libra_chunk_plan(libra_handle_t h, const int32_t* q_lens_host, const int32_t
   c.next_staging = k ^ 1;
   c.serial = serial;
   c.workspace = workspace_dev;
+  c.most_new = 0;
+  for (int32_t b = 0; b < batch; ++b) c.most_new = std::max(c.most_new, q_lens_host[b]);
   c.n_items = int32_t(plan.items.size());
   c.n_merges = int32_t(plan.merges.size());
   c.merges_off = merges_off;
@@ -194,81 +268,14 @@ int libra_chunk_plan(libra_handle_t h, const int32_t* q_lens_host, const int32_t
 
 int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
                      const int32_t* block_table, void* out, float* lse, void* error_word_dev, void* stream) {
-  if (!h || !q || !k_pages || !v_pages || !block_table || !out || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
-  if (q_stride < int64_t(h->cfg.num_q_heads) * h->cfg.head_dim || q_stride % 8 != 0) return LIBRA_INVALID_ARGUMENT;
-  auto off = [](const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; };
-  if (off(q, 16) || off(k_pages, 16) || off(v_pages, 16) || off(out, 16) || off(block_table, 4) || off(lse, 4) || off(error_word_dev, 4)) {
-    return LIBRA_INVALID_ARGUMENT;
-  }
-  // the kernels flush what is not normal to zero
-  if (!std::isnormal(h->scale_log2 * h->k_scale) || !std::isnormal(h->v_scale)) return LIBRA_INVALID_ARGUMENT;
-  libra_handle_s::Chunk& c = h->chunk;
-  if (!c.planned) return LIBRA_NOT_PLANNED;
-  if (c.n_items == 0) return LIBRA_OK;
-  DeviceGuard guard(h->cfg.device);
-  if (guard.err != cudaSuccess) return fail_cuda(h, guard.err);
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return attend(h, q, q_stride, k_pages, v_pages, block_table, nullptr, 0, out, lse, error_word_dev, stream);
+}
 
-  // whole pages: 64 channels with 128-byte swizzle as the tensor cores read them, or an 8-bit row as it is
-  const int row_bytes = h->fp8 ? h->cfg.head_dim : 128;
-  const CUtensorMapSwizzle swizzle = h->fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
-  CUtensorMap map_k, map_v;
-  int pos_head = 0, pos_page = 0, pos_token = 0;
-  int rc = libra::encode_pool_map(h, k_pages, row_bytes, h->cfg.page_size, swizzle, &map_k, &pos_head, &pos_page, &pos_token);
-  if (rc == LIBRA_OK) {
-    rc = libra::encode_pool_map(h, v_pages, row_bytes, h->cfg.page_size, swizzle, &map_v, &pos_head, &pos_page, &pos_token);
-  }
-  if (rc != LIBRA_OK) return rc;
-
-  uint8_t* ws = static_cast<uint8_t*>(c.workspace);
-  libra::ChunkParams p;
-  p.q = static_cast<const __nv_bfloat16*>(q);
-  p.q_stride = q_stride;
-  p.block_table = block_table;
-  p.out = static_cast<__nv_bfloat16*>(out);
-  p.lse = lse;
-  p.serial_at = reinterpret_cast<const uint32_t*>(ws);
-  p.items = reinterpret_cast<const int4*>(ws + kHeaderBytes);
-  p.partial_o = reinterpret_cast<float*>(ws + c.o_off);
-  p.partial_lse = reinterpret_cast<float*>(ws + c.lse_off);
-  p.error_word = static_cast<uint32_t*>(error_word_dev);
-  p.num_pages = h->cfg.num_pages;
-  p.serial = c.serial;
-  p.num_items = c.n_items;
-  p.num_q_heads = h->cfg.num_q_heads;
-  p.num_kv_heads = h->cfg.num_kv_heads;
-  p.group = h->group;
-  p.group_inverse = uint32_t((65536 + h->group - 1) / h->group);
-  p.block_table_ld = h->cfg.block_table_ld;
-  p.page_shift = h->cfg.page_size == 16 ? 4 : (h->cfg.page_size == 32 ? 5 : 6);
-  p.pos_head = pos_head;
-  p.pos_page = pos_page;
-  p.pos_token = pos_token;
-  p.scale_log2 = h->scale_log2 * h->k_scale;
-  p.v_scale = h->v_scale;
-  const int di = h->cfg.head_dim == 128 ? 1 : 0;
-  const ChunkBuild& b = kBuilds[di][h->fp8 ? 1 : 0];
-  const dim3 blocks(unsigned(p.num_kv_heads), unsigned(std::min(c.n_items, 65535)), unsigned((c.n_items + 65534) / 65535));
-  LIBRA_CUDA_TRY(h, launch(h->pdl, b.fn, blocks, unsigned(b.threads), size_t(b.smem), st, map_k, map_v, p));
-  ++h->launches;
-  if (c.n_merges > 0) {
-    libra::ChunkMergeParams m;
-    m.merges = reinterpret_cast<const int4*>(ws + c.merges_off);
-    m.serial_at = p.serial_at;
-    m.partial_o = p.partial_o;
-    m.partial_lse = p.partial_lse;
-    m.out = p.out;
-    m.lse = lse;
-    m.serial = c.serial;
-    m.num_q_heads = p.num_q_heads;
-    m.num_kv_heads = p.num_kv_heads;
-    m.group = p.group;
-    const dim3 grid(unsigned(c.n_merges * p.num_kv_heads), unsigned(libra::kChunkItemRows / libra::kChunkMergeWarps));
-    LIBRA_CUDA_TRY(h, launch(h->pdl, di ? libra::chunk_merge_kernel<128> : libra::chunk_merge_kernel<64>, grid,
-                             unsigned(libra::kChunkMergeWarps * 32), 0, st, m));
-    ++h->launches;
-  }
-  return LIBRA_OK;
+int libra_tree_attn(libra_handle_t h, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
+                    const int32_t* block_table, const uint32_t* mask, int32_t mask_ld, void* out, float* lse, void* error_word_dev,
+                    void* stream) {
+  if (!mask || mask_ld <= 0 || reinterpret_cast<uintptr_t>(mask) % 4 != 0) return LIBRA_INVALID_ARGUMENT;
+  return attend(h, q, q_stride, k_pages, v_pages, block_table, mask, mask_ld, out, lse, error_word_dev, stream);
 }
 
 }  // extern "C"

@@ -75,6 +75,8 @@ struct ChunkParams {
   int32_t pos_head, pos_page, pos_token;
   float scale_log2;           // sm_scale * log2(e) * k_scale
   float v_scale;
+  const uint32_t* mask;       // trees: [row of q][mask_ld], which new tokens of its sequence a token sees
+  int32_t mask_ld;
 };
 
 template <int D, bool kFp8>
@@ -346,9 +348,25 @@ __device__ __forceinline__ ChunkUnit load_unit(const ChunkParams& p) {
   return x;
 }
 
+// Which of the 128 tokens from kv0 on a token of a tree sees, as bits: all that were cached before the new ones (of which there
+// are `ctx`), of the new ones those that its row of the mask names, none from `sees` on.
+__device__ __forceinline__ void tree_bits(uint32_t (&seen)[4], const uint32_t* row, int mask_ld, int kv0, int ctx, int sees) {
+  const int j0 = kv0 - ctx, first = j0 >> 5, shift = j0 & 31;   // rounded down: words before the mask's first stand for cached tokens
+  auto word = [&](int k) { return k < 0 ? 0xffffffffu : (k < mask_ld ? __ldg(row + k) : 0u); };
+  uint32_t low = word(first);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t high = word(first + w + 1);
+    const int left = sees - kv0 - 32 * w;
+    seen[w] = __funnelshift_r(low, high, shift) & (left >= 32 ? 0xffffffffu : (left <= 0 ? 0u : (1u << left) - 1u));
+    low = high;
+  }
+}
+
 }  // namespace chunk
 
-template <int D, bool kFp8>
+// kTree: the new tokens of a sequence are not a chain but a tree, and see what p.mask says.
+template <int D, bool kFp8, bool kTree>
 __global__ void __launch_bounds__(ChunkShape<D, kFp8>::kThreads, 1)
 chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
              const __grid_constant__ ChunkParams p) {
@@ -405,11 +423,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       const int steps = x.steps_of(t), all_steps = x.steps;
       const int kv_pitch = solo ? 2 * kChunkKvTile : kChunkKvTile;
       int kv0 = x.kv_begin + (solo ? t * kChunkKvTile : 0), sees;
+      int mask_row = 0;          // trees: this row's of the mask,
+      const int ctx = x.ctx;     // and the first new token
       {
         const int tile_row = (solo ? 0 : t * kChunkTileRows) + row;   // row within the item
         int token, head;
         rows.at(p, tile_row, token, head);
         sees = tile_row < x.n_rows ? min(x.kv_end, x.ctx + token + 1) : 0;   // cached tokens this row sees
+        if (kTree && tile_row < x.n_rows) mask_row = x.q_start + token;
       }
       // ---- Q: 16 threads (8 at D = 64) bring a row
       if (all_steps > 0 && !(solo && t == 1)) {
@@ -472,10 +493,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         wait_ld();
 #pragma unroll
         for (int c = 0; c < 4; ++c) settle<32>(s + 32 * c);
-        const int limit = sees - kv0;
-        if (__any_sync(0xffffffffu, limit < kChunkKvTile)) {
+        if constexpr (kTree) {
+          if (kv0 + kChunkKvTile > ctx) {   // the same for all rows
+            uint32_t seen[4];
+            tree_bits(seen, p.mask + int64_t(mask_row) * p.mask_ld, p.mask_ld, kv0, ctx, sees);
 #pragma unroll
-          for (int c = 0; c < 128; ++c) s[c] = c < limit ? s[c] : -INFINITY;
+            for (int c = 0; c < 128; ++c) s[c] = (seen[c >> 5] >> (c & 31)) & 1u ? s[c] : -INFINITY;
+          }
+        } else {
+          const int limit = sees - kv0;
+          if (__any_sync(0xffffffffu, limit < kChunkKvTile)) {
+#pragma unroll
+            for (int c = 0; c < 128; ++c) s[c] = c < limit ? s[c] : -INFINITY;
+          }
         }
         auto row_max = [&] {
           float mx[4] = {s[0], s[1], s[2], s[3]};

@@ -104,6 +104,7 @@ struct libra_handle_s {
     uint32_t serial = 0;              // of the plan, also in the workspace
     void* workspace = nullptr;
     int32_t n_items = 0, n_merges = 0;
+    int32_t most_new = 0;             // new tokens of a sequence
     size_t merges_off = 0, lse_off = 0, o_off = 0;
     void* staging[2] = {nullptr, nullptr};   // pinned, grown when a plan needs more
     size_t staging_bytes[2] = {0, 0};

@@ -1,0 +1,273 @@
+// Block tables and slot maps made on the GPU: pages handed out to sequences that grow and taken back from those that shrink.
+//
+//   extend  sequence b of L_b tokens gets n_b more:  w_b = ceil((L_b + n_b) / P) - ceil(L_b / P) pages, in the order of the batch
+//           and of the pages; the k-th of them all is free[count - 1 - k].  Row q_offsets[b] + i is token t = L_b + i, in slot
+//           page(t / P) * P + t % P.
+//   trim    sequence b keeps its first m_b tokens: pages from ceil(m_b / P) on go back; the k-th of the F of them is
+//           free[count + F - 1 - k], so that what extend has taken trim puts back in the order it was.
+//
+// Integers only.  A token's page index follows from its position, and a page is new exactly where its first token is, so that one
+// pass over the rows writes positions, slots and block table; what it needs is the two prefix sums (rows and pages).
+//
+// One cluster of up to 8 blocks.  Every block computes the prefix sums of the whole batch for itself (up to 4096 sequences, four a
+// thread) into its shared memory - that is cheaper than handing them round - and the rows, or the pages that go back, are shared out
+// between the blocks, four rows a thread and step.  All checks are made on the sums before anything is written.  seq_lens and the
+// count change in place: the first block writes them once all have read them (cluster barrier).
+//
+// What bounds it: latency.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "libra.h"
+
+namespace libra {
+
+constexpr int kTablePerThread = 4;
+constexpr int kTableMaxThreads = 1024;
+constexpr int kTableMaxBatch = kTablePerThread * kTableMaxThreads;
+constexpr int kTableMaxBlocks = 8;   // of the cluster
+
+struct TableParams {
+  const int32_t* change;   // extend: new tokens of each sequence; trim: tokens that it keeps
+  int32_t* seq_lens;
+  int32_t* block_table;
+  int32_t* free_pages;
+  int32_t* free_count;
+  int32_t* q_offsets;      // extend only, as the next two, which may be null
+  int32_t* positions;
+  int32_t* slots;
+  uint32_t* error_word;
+  int64_t num_pages;
+  int32_t batch, block_table_ld, page_shift, max_rows;
+};
+
+namespace table {
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t n;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+struct Sums {
+  int64_t rows;    // may pass 32 bits where a call is refused
+  int32_t pages;   // as many as rows at most
+};
+
+// Exclusive prefix sums over the threads of the block, and the totals.
+__device__ __forceinline__ Sums block_scan(Sums mine, Sums& total) {
+  __shared__ Sums warp_sums[kTableMaxThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  Sums in = mine;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int64_t r = __shfl_up_sync(0xffffffffu, in.rows, off);
+    const int32_t g = __shfl_up_sync(0xffffffffu, in.pages, off);
+    if (lane >= off) {
+      in.rows += r;
+      in.pages += g;
+    }
+  }
+  if (lane == 31) warp_sums[warp] = in;
+  __syncthreads();
+  Sums before = {0, 0};
+  total = {0, 0};
+  for (int w = 0; w < warps; ++w) {
+    const Sums s = warp_sums[w];
+    if (w < warp) {
+      before.rows += s.rows;
+      before.pages += s.pages;
+    }
+    total.rows += s.rows;
+    total.pages += s.pages;
+  }
+  return {before.rows + in.rows - mine.rows, before.pages + in.pages - mine.pages};
+}
+
+// The last i in [0, n) with begins[i] <= x; begins[0] <= x.
+__device__ __forceinline__ int owner_of(const int32_t* begins, int n, int32_t x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (begins[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+}  // namespace table
+
+// grid = one cluster; dynamic shared memory: 3 * batch + 1 int32 (extend), 2 * batch (trim)
+__global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const TableParams p) {
+  using namespace table;
+  extern __shared__ int32_t sh[];
+  int32_t* const row_begin = sh;                       // [batch + 1]
+  int32_t* const page_begin = sh + p.batch + 1;        // [batch]
+  int32_t* const length = page_begin + p.batch;        // [batch], before
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const uint32_t rank = cluster_rank(), ranks = cluster_size();
+  const int b0 = threadIdx.x * kTablePerThread, P = 1 << p.page_shift;
+  const int64_t most = min(int64_t(p.block_table_ld) << p.page_shift, int64_t(0x7fffffff));   // that a row describes
+  const int32_t count = *p.free_count;
+  uint32_t bad = count < 0 || count > p.num_pages ? LIBRA_ERR_BAD_LENGTH : 0u;
+  int32_t len[kTablePerThread], add[kTablePerThread], want[kTablePerThread];
+  Sums mine = {0, 0};
+#pragma unroll
+  for (int i = 0; i < kTablePerThread; ++i) {
+    const bool live = b0 + i < p.batch;
+    len[i] = live ? p.seq_lens[b0 + i] : 0;
+    add[i] = live ? p.change[b0 + i] : 0;
+    if (len[i] < 0 || add[i] < 0) {
+      bad |= LIBRA_ERR_BAD_LENGTH;
+      len[i] = add[i] = 0;
+    }
+    if (int64_t(len[i]) + add[i] > most) {
+      bad |= LIBRA_ERR_PLAN_OVERFLOW;
+      add[i] = 0;
+    }
+    // 64 bits: a length within `most` may lie next to 2^31
+    want[i] = int32_t(((int64_t(len[i]) + add[i] + P - 1) >> p.page_shift) - ((int64_t(len[i]) + P - 1) >> p.page_shift));
+    mine.rows += add[i];
+    mine.pages += want[i];
+  }
+  Sums total;
+  Sums at = block_scan(mine, total);
+  if (total.rows > p.max_rows) bad |= LIBRA_ERR_PLAN_OVERFLOW;
+  else if (total.pages > count) bad |= LIBRA_ERR_NO_PAGES;
+  // every block comes to the same verdict
+  const bool refused = __syncthreads_or(int(bad)) != 0;
+  if (refused) {   // nothing changes, and the batch has no new rows
+    if (rank == 0) {
+      if (bad) atomicOr(p.error_word, bad);
+      for (int b = threadIdx.x; b <= p.batch; b += blockDim.x) p.q_offsets[b] = 0;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kTablePerThread; ++i) {
+    const int b = b0 + i;
+    if (b < p.batch) {
+      row_begin[b] = int32_t(at.rows);
+      page_begin[b] = at.pages;
+      length[b] = len[i];
+    }
+    at.rows += add[i];
+    at.pages += want[i];
+  }
+  const int32_t rows = int32_t(total.rows);
+  if (threadIdx.x == 0) row_begin[p.batch] = rows;
+  __syncthreads();
+  cluster_arrive();   // this block has read the lengths and the count
+  const bool vectors = ((reinterpret_cast<uintptr_t>(p.positions) | reinterpret_cast<uintptr_t>(p.slots)) & 15) == 0;
+  const int64_t step = int64_t(ranks) * blockDim.x * 4;
+  for (int64_t r0 = (int64_t(rank) * blockDim.x + threadIdx.x) * 4; r0 < rows; r0 += step) {
+    const int n = int(min(int64_t(4), rows - r0));
+    int b = owner_of(row_begin, p.batch, int32_t(r0));
+    int32_t pos[4], slot[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i < n) {
+        const int32_t r = int32_t(r0) + i;
+        while (r >= row_begin[b + 1]) ++b;   // past sequences without new tokens too
+        const int32_t L = length[b], page = (L + (r - row_begin[b])) >> p.page_shift;
+        const int32_t had = int32_t((int64_t(L) + P - 1) >> p.page_shift);
+        pos[i] = L + (r - row_begin[b]);
+        int32_t* const entry = p.block_table + int64_t(b) * p.block_table_ld + page;
+        const bool fresh = page >= had;
+        const int32_t id = fresh ? p.free_pages[count - 1 - (page_begin[b] + page - had)] : *entry;
+        slot[i] = int32_t(uint32_t(id) << p.page_shift) + (pos[i] & (P - 1));
+        if (fresh && (pos[i] & (P - 1)) == 0) *entry = id;   // its first token
+      }
+    }
+    if (vectors && n == 4) {
+      if (p.positions) *reinterpret_cast<int4*>(p.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      if (p.slots) *reinterpret_cast<int4*>(p.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i < n && p.positions) p.positions[r0 + i] = pos[i];
+        if (i < n && p.slots) p.slots[r0 + i] = slot[i];
+      }
+    }
+  }
+  cluster_wait();
+  if (rank == 0) {
+#pragma unroll
+    for (int i = 0; i < kTablePerThread; ++i) {
+      if (b0 + i < p.batch && add[i] > 0) p.seq_lens[b0 + i] = len[i] + add[i];
+    }
+    for (int b = threadIdx.x; b <= p.batch; b += blockDim.x) p.q_offsets[b] = row_begin[b];
+    if (threadIdx.x == 0) *p.free_count = count - total.pages;
+  }
+}
+
+__global__ void __launch_bounds__(kTableMaxThreads) cache_trim_kernel(const TableParams p) {
+  using namespace table;
+  extern __shared__ int32_t sh[];
+  int32_t* const page_begin = sh;              // [batch]
+  int32_t* const left = sh + p.batch;          // [batch]: pages that stay
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const uint32_t rank = cluster_rank(), ranks = cluster_size();
+  const int b0 = threadIdx.x * kTablePerThread, P = 1 << p.page_shift;
+  const int64_t most = int64_t(p.block_table_ld) << p.page_shift;
+  const int32_t count = *p.free_count;
+  uint32_t bad = count < 0 || count > p.num_pages ? LIBRA_ERR_BAD_LENGTH : 0u;
+  int32_t len[kTablePerThread], keep[kTablePerThread], stay[kTablePerThread], gone[kTablePerThread];
+  Sums mine = {0, 0};   // rows: the pages once more, in 64 bits
+#pragma unroll
+  for (int i = 0; i < kTablePerThread; ++i) {
+    const bool live = b0 + i < p.batch;
+    len[i] = live ? p.seq_lens[b0 + i] : 0;
+    keep[i] = live ? p.change[b0 + i] : 0;
+    if (keep[i] < 0 || keep[i] > len[i] || len[i] > most) {
+      bad |= LIBRA_ERR_BAD_LENGTH;
+      len[i] = keep[i] = 0;
+    }
+    stay[i] = int32_t((int64_t(keep[i]) + P - 1) >> p.page_shift);
+    gone[i] = int32_t((int64_t(len[i]) + P - 1) >> p.page_shift) - stay[i];
+    mine.rows += gone[i];
+    mine.pages += gone[i];
+  }
+  Sums total;
+  Sums at = block_scan(mine, total);
+  if (count + total.rows > p.num_pages) bad |= LIBRA_ERR_BAD_LENGTH;   // more pages than there are
+  const bool refused = __syncthreads_or(int(bad)) != 0;
+  if (refused) {
+    if (rank == 0 && bad) atomicOr(p.error_word, bad);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kTablePerThread; ++i) {
+    if (b0 + i < p.batch) {
+      page_begin[b0 + i] = at.pages;
+      left[b0 + i] = stay[i];
+    }
+    at.pages += gone[i];
+  }
+  __syncthreads();
+  cluster_arrive();
+  const int64_t step = int64_t(ranks) * blockDim.x;
+  for (int64_t k = int64_t(rank) * blockDim.x + threadIdx.x; k < total.pages; k += step) {
+    const int b = owner_of(page_begin, p.batch, int32_t(k));
+    p.free_pages[count + total.pages - 1 - k] = p.block_table[int64_t(b) * p.block_table_ld + left[b] + (k - page_begin[b])];
+  }
+  cluster_wait();
+  if (rank == 0) {
+#pragma unroll
+    for (int i = 0; i < kTablePerThread; ++i) {
+      if (b0 + i < p.batch && keep[i] != len[i]) p.seq_lens[b0 + i] = keep[i];
+    }
+    if (threadIdx.x == 0) *p.free_count = count + total.pages;
+  }
+}
+
+}  // namespace libra
