@@ -40,47 +40,56 @@ bool rows_apart(int64_t n_tokens, int32_t n_heads, int32_t head_dim, int64_t tok
 
 bool wide_rows(const void* p, int64_t token, int64_t head, int v) { return aligned(p, 16) && token % v == 0 && head % v == 0; }
 
-// How a row is held by a group of lanes, or that it goes through shared memory (false).
-bool lay_out(NormParams* p, bool wide, int v) {
+// How a row is held by a group of lanes: the elements of a vector (0: the row goes through shared memory).  v: those of 16 bytes.
+int lay_out(NormParams* p, bool wide, int v) {
   const int R = p->rope.rotary_dim, D = p->head_dim;
   const bool half = p->rope.layout == LIBRA_ROPE_HALF;
-  if (!wide || D % v != 0 || (half ? R / 2 : R) % v != 0) return false;
-  const int turning = half ? R / (2 * v) : 0, rest = half ? D - R : D;
-  p->items = turning + (rest + 2 * v - 1) / (2 * v);
-  if (p->items > 32) return false;
+  if (!wide) return 0;
+  if (v == 8 && half && R % 16 == 8) v = 4;   // 8 bytes: R / 2 is an odd multiple of four elements
+  if (D % v != 0 || R % (half ? 2 * v : v) != 0) return 0;
+  p->items = half ? R / (2 * v) + ((D - R) / v + 1) / 2 : (D / v + 1) / 2;
+  if (p->items > 32) return 0;
   for (p->lanes = 1; p->lanes < p->items; p->lanes *= 2) {}
-  return true;
+  return v;
 }
 
-// Units of every kind and of a token; false: more than 32 bits count
-void count_units(NormParams* p, bool by_lanes) {
-  const int rows = by_lanes ? libra::kNormRows * (32 / p->lanes) : 1;
-  p->units = 0;
-  for (NormKind& k : p->kind) p->units += k.units = (k.n_heads + rows - 1) / rows;
+// Steps of every kind and of a token: the rows that a warp holds at once, or one
+void count_steps(NormParams* p, bool by_lanes) {
+  const int rows = by_lanes ? 32 / p->lanes : 1;
+  p->steps = 0;
+  for (NormKind& k : p->kind) p->steps += k.steps = (k.n_heads + rows - 1) / rows;
 }
 
-unsigned blocks_for(int64_t units, int warps, int64_t most) {
-  return unsigned(std::max<int64_t>(1, std::min<int64_t>((units + warps - 1) / warps, most)));
+unsigned blocks_for(int64_t steps, int warps, int64_t most) {
+  return unsigned(std::max<int64_t>(1, std::min<int64_t>((steps + warps - 1) / warps, most)));
 }
 
 typedef void (*NormFn)(NormParams);
 
+// v: the elements of a vector where a group of lanes holds a row, else 0
 template <typename T, int V>
-NormFn apply_fn(bool by_lanes, bool wide, bool half) {
-  if (by_lanes) return half ? libra::norm_rope_kernel<T, T, true, false> : libra::norm_rope_kernel<T, T, false, false>;
+NormFn apply_fn(int v, bool wide, bool half) {
+  if constexpr (V == 8) {
+    if (v == 4) return libra::norm_rope_kernel<T, T, 4, true, false>;
+  }
+  if (v) return half ? libra::norm_rope_kernel<T, T, V, true, false> : libra::norm_rope_kernel<T, T, V, false, false>;
   if (wide) return half ? libra::norm_rope_any_kernel<T, T, V, true, true, false> : libra::norm_rope_any_kernel<T, T, V, true, false, false>;
   return half ? libra::norm_rope_any_kernel<T, T, 1, false, true, false> : libra::norm_rope_any_kernel<T, T, 1, false, false, false>;
 }
 template <typename T, int V>
-NormFn gradient_fn(bool by_lanes, bool wide, bool half) {
-  if (by_lanes) return half ? libra::norm_rope_gradient_kernel<T, true> : libra::norm_rope_gradient_kernel<T, false>;
+NormFn gradient_fn(int v, bool wide, bool half) {
+  if constexpr (V == 8) {
+    if (v == 4) return libra::norm_rope_gradient_kernel<T, 4, true>;
+  }
+  if (v) return half ? libra::norm_rope_gradient_kernel<T, V, true> : libra::norm_rope_gradient_kernel<T, V, false>;
   if (wide) return half ? libra::norm_rope_gradient_any_kernel<T, V, true, true> : libra::norm_rope_gradient_any_kernel<T, V, true, false>;
   return half ? libra::norm_rope_gradient_any_kernel<T, 1, false, true> : libra::norm_rope_gradient_any_kernel<T, 1, false, false>;
 }
 template <typename P>
-NormFn append_fn(bool by_lanes, bool half) {   // the handle's strides and addresses are multiples of 16 bytes
+NormFn append_fn(int v, bool half) {   // the handle's strides and addresses are multiples of 16 bytes
   typedef __nv_bfloat16 T;
-  if (by_lanes) return half ? libra::norm_rope_kernel<T, P, true, true> : libra::norm_rope_kernel<T, P, false, true>;
+  if (v == 4) return libra::norm_rope_kernel<T, P, 4, true, true>;
+  if (v) return half ? libra::norm_rope_kernel<T, P, 8, true, true> : libra::norm_rope_kernel<T, P, 8, false, true>;
   return half ? libra::norm_rope_any_kernel<T, P, 8, true, true, true> : libra::norm_rope_any_kernel<T, P, 8, true, false, true>;
 }
 
@@ -147,13 +156,14 @@ int libra_norm_rope_apply(int32_t device, const libra_rope_t* rope, const libra_
   if (sm_count(device, &n_sm) != LIBRA_OK) return LIBRA_CUDA_ERROR;
   set_common(&p, rope, positions, n_tokens, head_dim, eps);
   wide = wide && head_dim % v == 0;
-  const bool by_lanes = lay_out(&p, wide, v), half = p.rope.layout == LIBRA_ROPE_HALF;
-  count_units(&p, by_lanes);
-  const NormFn fn = dtype == LIBRA_ROPE_BF16  ? apply_fn<__nv_bfloat16, 8>(by_lanes, wide, half)
-                    : dtype == LIBRA_ROPE_F16 ? apply_fn<__half, 8>(by_lanes, wide, half)
-                                              : apply_fn<float, 4>(by_lanes, wide, half);
+  const int vec = lay_out(&p, wide, v);
+  const bool by_lanes = vec != 0, half = p.rope.layout == LIBRA_ROPE_HALF;
+  count_steps(&p, by_lanes);
+  const NormFn fn = dtype == LIBRA_ROPE_BF16  ? apply_fn<__nv_bfloat16, 8>(vec, wide, half)
+                    : dtype == LIBRA_ROPE_F16 ? apply_fn<__half, 8>(vec, wide, half)
+                                              : apply_fn<float, 4>(vec, wide, half);
   const int warps = by_lanes ? libra::kNormWarps : libra::kNormAnyWarps;
-  const unsigned grid = blocks_for(n_tokens * p.units, warps, int64_t(n_sm) * (by_lanes ? 8 : 16));
+  const unsigned grid = blocks_for(n_tokens * p.steps, warps, int64_t(n_sm) * (by_lanes ? libra::kNormBlocks : 16));
   fn<<<grid, warps * 32, by_lanes ? 0 : size_t(warps) * head_dim * sizeof(float), static_cast<cudaStream_t>(stream)>>>(p);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? LIBRA_OK : fail_cuda(nullptr, e);
@@ -164,7 +174,7 @@ int libra_norm_rope_workspace_size(int32_t device, int32_t head_dim, size_t* byt
   if (head_dim % 2 != 0 || head_dim > 1024) return LIBRA_UNSUPPORTED_SHAPE;
   int n_sm = 0;
   if (sm_count(device, &n_sm) != LIBRA_OK) return LIBRA_CUDA_ERROR;
-  *bytes = size_t(n_sm) * kMostBlocks * head_dim * sizeof(float);
+  *bytes = size_t(n_sm) * kMostBlocks * 2 * head_dim * sizeof(float);
   return LIBRA_OK;
 }
 
@@ -217,35 +227,35 @@ int libra_norm_rope_gradient(int32_t device, const libra_rope_t* rope, const lib
   if (guard.err != cudaSuccess) return fail_cuda(nullptr, guard.err);
   int n_sm = 0;
   if (sm_count(device, &n_sm) != LIBRA_OK) return LIBRA_CUDA_ERROR;
-  if (workspace_bytes < size_t(n_sm) * kMostBlocks * head_dim * sizeof(float)) return LIBRA_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < size_t(n_sm) * kMostBlocks * 2 * head_dim * sizeof(float)) return LIBRA_WORKSPACE_TOO_SMALL;
   set_common(&p, rope, positions, n_tokens, head_dim, eps);
   p.partial = static_cast<float*>(workspace_dev);
   wide = wide && head_dim % v == 0;
-  const bool by_lanes = lay_out(&p, wide, v), half = p.rope.layout == LIBRA_ROPE_HALF;
-  count_units(&p, by_lanes);
-  const int warps = by_lanes ? libra::kNormWarps : libra::kNormAnyWarps;
-  // the blocks that are resident at once, shared out to q and k by their rows
-  const int64_t most = int64_t(n_sm) * (by_lanes ? 2 : kMostBlocks);
-  const unsigned first = blocks_for(n_tokens * p.kind[0].units, warps, k ? std::max<int64_t>(1, most * p.kind[0].units / p.units) : most);
-  const unsigned second = k ? blocks_for(n_tokens * p.kind[1].units, warps, std::max<int64_t>(1, most - most * p.kind[0].units / p.units)) : 0;
-  p.first_blocks = int32_t(first);
-  const NormFn fn = dtype == LIBRA_ROPE_BF16  ? gradient_fn<__nv_bfloat16, 8>(by_lanes, wide, half)
-                    : dtype == LIBRA_ROPE_F16 ? gradient_fn<__half, 8>(by_lanes, wide, half)
-                                              : gradient_fn<float, 4>(by_lanes, wide, half);
+  const int vec = lay_out(&p, wide, v);
+  const bool by_lanes = vec != 0, half = p.rope.layout == LIBRA_ROPE_HALF;
+  count_steps(&p, by_lanes);
+  const int warps = !by_lanes ? libra::kNormAnyWarps
+                              : (dtype == LIBRA_ROPE_F32 ? libra::kNormGradThreads<float> : libra::kNormGradThreads<__half>) / 32;
+  const unsigned blocks = blocks_for(n_tokens * p.steps, warps, int64_t(n_sm) * (by_lanes ? 1 : kMostBlocks));
+  const NormFn fn = dtype == LIBRA_ROPE_BF16  ? gradient_fn<__nv_bfloat16, 8>(vec, wide, half)
+                    : dtype == LIBRA_ROPE_F16 ? gradient_fn<__half, 8>(vec, wide, half)
+                                              : gradient_fn<float, 4>(vec, wide, half);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const size_t smem = size_t(warps) * head_dim * sizeof(float) * (by_lanes ? 1 : 3);
+  const int kinds = k ? 2 : 1;
+  const size_t row = size_t(head_dim) * sizeof(float);
+  const size_t smem = size_t(warps) * (by_lanes ? std::max<size_t>(libra::kNormGradAhead * libra::kNormGradStepBytes, kinds * row) : (2 + kinds) * row);
   if (smem > 40 * 1024) {   // beside the static part
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
     if (e != cudaSuccess) return fail_cuda(nullptr, e);
   }
-  fn<<<first + second, warps * 32, smem, st>>>(p);
+  fn<<<blocks, warps * 32, smem, st>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return fail_cuda(nullptr, e);
   s.partial = p.partial;
   s.head_dim = head_dim;
-  s.begin[1] = int32_t(first);
-  s.begin[2] = int32_t(first + second);
-  e = libra::launch(true, 1, libra::norm_sum_kernel, dim3(unsigned(head_dim + 31) / 32, k ? 2 : 1), 32 * libra::kNormSumSlices, 0, st, s);
+  s.channels = kinds * head_dim;
+  s.blocks = int32_t(blocks);
+  e = libra::launch(true, 1, libra::norm_sum_kernel, dim3(unsigned(s.channels + 31) / 32), 32 * libra::kNormSumSlices, 0, st, s);
   return e == cudaSuccess ? LIBRA_OK : fail_cuda(nullptr, e);
 }
 
@@ -300,11 +310,12 @@ int libra_norm_rope_append(libra_handle_t h, const libra_rope_t* rope, const voi
   p.k_inv_scale = 1.f / h->k_scale;
   p.v_inv_scale = 1.f / h->v_scale;
   p.page_shift = h->cfg.page_size == 16 ? 4 : (h->cfg.page_size == 32 ? 5 : 6);
-  const bool by_lanes = lay_out(&p, true, 8), half = p.rope.layout == LIBRA_ROPE_HALF;
-  count_units(&p, by_lanes);
-  const NormFn fn = h->fp8 ? append_fn<uint8_t>(by_lanes, half) : append_fn<__nv_bfloat16>(by_lanes, half);
+  const int vec = lay_out(&p, true, 8);
+  const bool by_lanes = vec != 0, half = p.rope.layout == LIBRA_ROPE_HALF;
+  count_steps(&p, by_lanes);
+  const NormFn fn = h->fp8 ? append_fn<uint8_t>(vec, half) : append_fn<__nv_bfloat16>(vec, half);
   const int warps = by_lanes ? libra::kNormWarps : libra::kNormAnyWarps;
-  const unsigned grid = blocks_for(int64_t(max_rows) * p.units, warps, int64_t(h->n_sm_dev) * (by_lanes ? 8 : 16));
+  const unsigned grid = blocks_for(int64_t(max_rows) * p.steps, warps, int64_t(h->n_sm_dev) * (by_lanes ? libra::kNormBlocks : 16));
   LIBRA_CUDA_TRY(h, libra::launch(h->pdl, 1, fn, dim3(grid), unsigned(warps * 32), by_lanes ? 0 : size_t(warps) * D * sizeof(float),
                                   static_cast<cudaStream_t>(stream), p));
   ++h->launches;

@@ -172,20 +172,31 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const Ta
   for (int64_t r0 = (int64_t(rank) * blockDim.x + threadIdx.x) * 4; r0 < rows; r0 += step) {
     const int n = int(min(int64_t(4), rows - r0));
     int b = owner_of(row_begin, p.batch, int32_t(r0));
-    int32_t pos[4], slot[4];
+    int32_t pos[4], slot[4], id[4];
+    int32_t* entry[4];   // of the block table, where this row writes it
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) {   // the four loads are on their way together
+      entry[i] = nullptr;
       if (i < n) {
         const int32_t r = int32_t(r0) + i;
         while (r >= row_begin[b + 1]) ++b;   // past sequences without new tokens too
-        const int32_t L = length[b], page = (L + (r - row_begin[b])) >> p.page_shift;
-        const int32_t had = int32_t((int64_t(L) + P - 1) >> p.page_shift);
+        const int32_t L = length[b];
         pos[i] = L + (r - row_begin[b]);
-        int32_t* const entry = p.block_table + int64_t(b) * p.block_table_ld + page;
-        const bool fresh = page >= had;
-        const int32_t id = fresh ? p.free_pages[count - 1 - (page_begin[b] + page - had)] : *entry;
-        slot[i] = int32_t(uint32_t(id) << p.page_shift) + (pos[i] & (P - 1));
-        if (fresh && (pos[i] & (P - 1)) == 0) *entry = id;   // its first token
+        const int32_t page = pos[i] >> p.page_shift, had = int32_t((int64_t(L) + P - 1) >> p.page_shift);
+        int32_t* const at = p.block_table + int64_t(b) * p.block_table_ld + page;
+        const int32_t* from = at;
+        if (page >= had) {
+          from = p.free_pages + (count - 1 - (page_begin[b] + page - had));
+          if ((pos[i] & (P - 1)) == 0) entry[i] = at;   // its first token
+        }
+        id[i] = *from;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i < n) {
+        slot[i] = int32_t(uint32_t(id[i]) << p.page_shift) + (pos[i] & (P - 1));
+        if (entry[i]) *entry[i] = id[i];
       }
     }
     if (vectors && n == 4) {
