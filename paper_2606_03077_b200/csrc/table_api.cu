@@ -74,7 +74,7 @@ int libra_cache_extend(libra_handle_t h, const int32_t* new_tokens, int32_t* seq
   p.positions = positions;
   p.slots = slots;
   p.max_rows = max_rows;
-  return launch_table(h, libra::cache_extend_kernel, p, (int64_t(max_rows) + 3) / 4, (3 * size_t(batch) + 1) * sizeof(int32_t), stream);
+  return launch_table(h, libra::cache_extend_kernel, p, max_rows, (3 * size_t(batch) + 1) * sizeof(int32_t), stream);
 }
 
 int libra_cache_trim(libra_handle_t h, const int32_t* keep_lens, int32_t* seq_lens, int32_t* block_table, int32_t batch,
@@ -84,7 +84,7 @@ int libra_cache_trim(libra_handle_t h, const int32_t* keep_lens, int32_t* seq_le
   if (rc != LIBRA_OK) return rc;
   if (batch == 0) return LIBRA_OK;
   const int64_t pages = std::min(int64_t(batch) * h->cfg.block_table_ld, h->cfg.num_pages);
-  return launch_table(h, libra::cache_trim_kernel, p, (pages + 7) / 8, 2 * size_t(batch) * sizeof(int32_t), stream);
+  return launch_table(h, libra::cache_trim_kernel, p, (pages + 15) / 16, 2 * size_t(batch) * sizeof(int32_t), stream);
 }
 
 }  // extern "C"

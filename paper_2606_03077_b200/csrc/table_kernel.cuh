@@ -11,7 +11,7 @@
 //
 // One cluster of up to 8 blocks.  Every block computes the prefix sums of the whole batch for itself (up to 4096 sequences, four a
 // thread) into its shared memory - that is cheaper than handing them round - and the rows, or the pages that go back, are shared out
-// between the blocks, four rows a thread and step.  All checks are made on the sums before anything is written.  seq_lens and the
+// between the blocks.  All checks are made on the sums before anything is written.  seq_lens and the
 // count change in place: the first block writes them once all have read them (cluster barrier).
 //
 // What bounds it: latency.
@@ -28,6 +28,7 @@ constexpr int kTablePerThread = 4;
 constexpr int kTableMaxThreads = 1024;
 constexpr int kTableMaxBatch = kTablePerThread * kTableMaxThreads;
 constexpr int kTableMaxBlocks = 8;   // of the cluster
+constexpr int kTableRows = 8;        // of a thread and turn in long batches; no more than a page has tokens
 
 struct TableParams {
   const int32_t* change;   // extend: new tokens of each sequence; trim: tokens that it keeps
@@ -63,34 +64,49 @@ struct Sums {
   int32_t pages;   // as many as rows at most
 };
 
-// Exclusive prefix sums over the threads of the block, and the totals.
-__device__ __forceinline__ Sums block_scan(Sums mine, Sums& total) {
-  __shared__ Sums warp_sums[kTableMaxThreads / 32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+// Exclusive prefix sums over the threads of the block, and the totals.  Of the warps the first `busy` have something.
+__device__ __forceinline__ Sums block_scan(Sums mine, int busy, Sums& total) {
+  __shared__ Sums warp_sums[kTableMaxThreads / 32 + 1];   // the total behind the last
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Sums in = mine;
+  if (warp < busy) {
 #pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const int64_t r = __shfl_up_sync(0xffffffffu, in.rows, off);
-    const int32_t g = __shfl_up_sync(0xffffffffu, in.pages, off);
-    if (lane >= off) {
-      in.rows += r;
-      in.pages += g;
+    for (int off = 1; off < 32; off <<= 1) {
+      const int64_t r = __shfl_up_sync(0xffffffffu, in.rows, off);
+      const int32_t g = __shfl_up_sync(0xffffffffu, in.pages, off);
+      if (lane >= off) {
+        in.rows += r;
+        in.pages += g;
+      }
     }
+    if (lane == 31) warp_sums[warp] = in;
   }
-  if (lane == 31) warp_sums[warp] = in;
   __syncthreads();
-  Sums before = {0, 0};
-  total = {0, 0};
-  for (int w = 0; w < warps; ++w) {
-    const Sums s = warp_sums[w];
-    if (w < warp) {
-      before.rows += s.rows;
-      before.pages += s.pages;
+  if (warp == 0) {   // the warps' sums become what lies before each
+    const Sums own = lane < busy ? warp_sums[lane] : Sums{0, 0};
+    Sums upto = own;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int64_t r = __shfl_up_sync(0xffffffffu, upto.rows, off);
+      const int32_t g = __shfl_up_sync(0xffffffffu, upto.pages, off);
+      if (lane >= off) {
+        upto.rows += r;
+        upto.pages += g;
+      }
     }
-    total.rows += s.rows;
-    total.pages += s.pages;
+    __syncwarp();
+    warp_sums[lane] = {upto.rows - own.rows, upto.pages - own.pages};
+    if (lane == 31) warp_sums[32] = upto;
   }
+  __syncthreads();
+  total = warp_sums[32];
+  const Sums before = warp_sums[warp];
   return {before.rows + in.rows - mine.rows, before.pages + in.pages - mine.pages};
+}
+
+// ceil(len / page size) of a length that is not negative
+__device__ __forceinline__ int32_t pages_of(int32_t len, int page_shift) {
+  return int32_t((uint32_t(len) + (1u << page_shift) - 1) >> page_shift);
 }
 
 // The last i in [0, n) with begins[i] <= x; begins[0] <= x.
@@ -130,17 +146,16 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const Ta
       bad |= LIBRA_ERR_BAD_LENGTH;
       len[i] = add[i] = 0;
     }
-    if (int64_t(len[i]) + add[i] > most) {
+    if (int64_t(len[i]) + add[i] > most) {   // a sum that is left fits 31 bits
       bad |= LIBRA_ERR_PLAN_OVERFLOW;
       add[i] = 0;
     }
-    // 64 bits: a length within `most` may lie next to 2^31
-    want[i] = int32_t(((int64_t(len[i]) + add[i] + P - 1) >> p.page_shift) - ((int64_t(len[i]) + P - 1) >> p.page_shift));
+    want[i] = pages_of(len[i] + add[i], p.page_shift) - pages_of(len[i], p.page_shift);
     mine.rows += add[i];
     mine.pages += want[i];
   }
   Sums total;
-  Sums at = block_scan(mine, total);
+  Sums at = block_scan(mine, (p.batch + 32 * kTablePerThread - 1) / (32 * kTablePerThread), total);
   if (total.rows > p.max_rows) bad |= LIBRA_ERR_PLAN_OVERFLOW;
   else if (total.pages > count) bad |= LIBRA_ERR_NO_PAGES;
   // every block comes to the same verdict
@@ -166,51 +181,51 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const Ta
   const int32_t rows = int32_t(total.rows);
   if (threadIdx.x == 0) row_begin[p.batch] = rows;
   __syncthreads();
-  cluster_arrive();   // this block has read the lengths and the count
-  const bool vectors = ((reinterpret_cast<uintptr_t>(p.positions) | reinterpret_cast<uintptr_t>(p.slots)) & 15) == 0;
-  const int64_t step = int64_t(ranks) * blockDim.x * 4;
-  for (int64_t r0 = (int64_t(rank) * blockDim.x + threadIdx.x) * 4; r0 < rows; r0 += step) {
-    const int n = int(min(int64_t(4), rows - r0));
+  if (ranks > 1) cluster_arrive();   // this block has read the lengths and the count
+  // A row a thread while there are threads enough, else kTableRows, with whole vectors written where the arrays lie on them.
+  const int64_t threads = int64_t(ranks) * blockDim.x;
+  const int per = rows > threads ? kTableRows : 1;
+  const bool vectors = per > 1 && ((reinterpret_cast<uintptr_t>(p.positions) | reinterpret_cast<uintptr_t>(p.slots)) & 15) == 0;
+  for (int64_t r0 = (int64_t(rank) * blockDim.x + threadIdx.x) * per; r0 < rows; r0 += threads * per) {
+    const int n = int(min(int64_t(per), rows - r0));
     int b = owner_of(row_begin, p.batch, int32_t(r0));
-    int32_t pos[4], slot[4], id[4];
-    int32_t* entry[4];   // of the block table, where this row writes it
+    int32_t pos[kTableRows], slot[kTableRows];
+    for (int i = 0; i < n; ++b) {   // the rows of one sequence, in two pages at most; sequences without new tokens have none
+      const int m = min(n - i, row_begin[b + 1] - (int32_t(r0) + i));
+      if (m == 0) continue;
+      const int32_t L = length[b], first = L + (int32_t(r0) + i - row_begin[b]);
+      const int32_t page0 = first >> p.page_shift, page1 = (first + m - 1) >> p.page_shift, had = pages_of(L, p.page_shift);
+      int32_t* const row = p.block_table + int64_t(b) * p.block_table_ld;
+      // a page's id comes from the stack where the page is new, and is entered by the thread that has the page's first token
+      const int32_t* const stack = p.free_pages + (count - 1 - page_begin[b] + had);
+      const int32_t id0 = page0 >= had ? stack[-page0] : row[page0];
+      const int32_t id1 = page1 == page0 ? id0 : (page1 >= had ? stack[-page1] : row[page1]);
+      if (page0 >= had && (first & (P - 1)) == 0) row[page0] = id0;
+      if (page1 != page0 && page1 >= had) row[page1] = id1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {   // the four loads are on their way together
-      entry[i] = nullptr;
-      if (i < n) {
-        const int32_t r = int32_t(r0) + i;
-        while (r >= row_begin[b + 1]) ++b;   // past sequences without new tokens too
-        const int32_t L = length[b];
-        pos[i] = L + (r - row_begin[b]);
-        const int32_t page = pos[i] >> p.page_shift, had = int32_t((int64_t(L) + P - 1) >> p.page_shift);
-        int32_t* const at = p.block_table + int64_t(b) * p.block_table_ld + page;
-        const int32_t* from = at;
-        if (page >= had) {
-          from = p.free_pages + (count - 1 - (page_begin[b] + page - had));
-          if ((pos[i] & (P - 1)) == 0) entry[i] = at;   // its first token
+      for (int k = 0; k < kTableRows; ++k) {
+        if (k >= i && k < i + m) {
+          pos[k] = first + (k - i);
+          slot[k] = int32_t(uint32_t(pos[k] >> p.page_shift == page0 ? id0 : id1) << p.page_shift) + (pos[k] & (P - 1));
         }
-        id[i] = *from;
       }
+      i += m;
     }
+    if (vectors && n == kTableRows) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i < n) {
-        slot[i] = int32_t(uint32_t(id[i]) << p.page_shift) + (pos[i] & (P - 1));
-        if (entry[i]) *entry[i] = id[i];
+      for (int k = 0; k < kTableRows; k += 4) {
+        if (p.positions) *reinterpret_cast<int4*>(p.positions + r0 + k) = make_int4(pos[k], pos[k + 1], pos[k + 2], pos[k + 3]);
+        if (p.slots) *reinterpret_cast<int4*>(p.slots + r0 + k) = make_int4(slot[k], slot[k + 1], slot[k + 2], slot[k + 3]);
       }
-    }
-    if (vectors && n == 4) {
-      if (p.positions) *reinterpret_cast<int4*>(p.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-      if (p.slots) *reinterpret_cast<int4*>(p.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i < n && p.positions) p.positions[r0 + i] = pos[i];
-        if (i < n && p.slots) p.slots[r0 + i] = slot[i];
+      for (int k = 0; k < kTableRows; ++k) {
+        if (k < n && p.positions) p.positions[r0 + k] = pos[k];
+        if (k < n && p.slots) p.slots[r0 + k] = slot[k];
       }
     }
   }
-  cluster_wait();
+  if (ranks > 1) cluster_wait();
   if (rank == 0) {
 #pragma unroll
     for (int i = 0; i < kTablePerThread; ++i) {
@@ -228,7 +243,7 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_trim_kernel(const Tabl
   int32_t* const left = sh + p.batch;          // [batch]: pages that stay
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint32_t rank = cluster_rank(), ranks = cluster_size();
-  const int b0 = threadIdx.x * kTablePerThread, P = 1 << p.page_shift;
+  const int b0 = threadIdx.x * kTablePerThread;
   const int64_t most = int64_t(p.block_table_ld) << p.page_shift;
   const int32_t count = *p.free_count;
   uint32_t bad = count < 0 || count > p.num_pages ? LIBRA_ERR_BAD_LENGTH : 0u;
@@ -243,13 +258,13 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_trim_kernel(const Tabl
       bad |= LIBRA_ERR_BAD_LENGTH;
       len[i] = keep[i] = 0;
     }
-    stay[i] = int32_t((int64_t(keep[i]) + P - 1) >> p.page_shift);
-    gone[i] = int32_t((int64_t(len[i]) + P - 1) >> p.page_shift) - stay[i];
+    stay[i] = pages_of(keep[i], p.page_shift);
+    gone[i] = pages_of(len[i], p.page_shift) - stay[i];
     mine.rows += gone[i];
     mine.pages += gone[i];
   }
   Sums total;
-  Sums at = block_scan(mine, total);
+  Sums at = block_scan(mine, (p.batch + 32 * kTablePerThread - 1) / (32 * kTablePerThread), total);
   if (count + total.rows > p.num_pages) bad |= LIBRA_ERR_BAD_LENGTH;   // more pages than there are
   const bool refused = __syncthreads_or(int(bad)) != 0;
   if (refused) {
@@ -265,13 +280,13 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_trim_kernel(const Tabl
     at.pages += gone[i];
   }
   __syncthreads();
-  cluster_arrive();
+  if (ranks > 1) cluster_arrive();
   const int64_t step = int64_t(ranks) * blockDim.x;
   for (int64_t k = int64_t(rank) * blockDim.x + threadIdx.x; k < total.pages; k += step) {
     const int b = owner_of(page_begin, p.batch, int32_t(k));
     p.free_pages[count + total.pages - 1 - k] = p.block_table[int64_t(b) * p.block_table_ld + left[b] + (k - page_begin[b])];
   }
-  cluster_wait();
+  if (ranks > 1) cluster_wait();
   if (rank == 0) {
 #pragma unroll
     for (int i = 0; i < kTablePerThread; ++i) {
