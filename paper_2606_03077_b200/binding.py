@@ -91,8 +91,8 @@ class NormRows(C.Structure):
     @classmethod
     def of(cls, x, weight, out) -> "NormRows":
         """From arrays [tokens, heads, head_dim] that know their address and strides, as tensors do."""
-        return cls(x.data_ptr(), out.data_ptr(), weight.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1),
-                   x.shape[1], 0)
+        xs, os = x.stride(), out.stride()
+        return cls(x.data_ptr(), out.data_ptr(), weight.data_ptr(), xs[0], xs[1], os[0], os[1], x.shape[1], 0)
 
 
 class NormGrads(C.Structure):
@@ -104,8 +104,9 @@ class NormGrads(C.Structure):
 
     @classmethod
     def of(cls, x, grad_out, weight, grad_x, grad_weight) -> "NormGrads":
-        return cls(x.data_ptr(), grad_out.data_ptr(), weight.data_ptr(), grad_x.data_ptr(), grad_weight.data_ptr(), x.stride(0),
-                   x.stride(1), grad_out.stride(0), grad_out.stride(1), grad_x.stride(0), grad_x.stride(1), x.shape[1], 0)
+        xs, gs, os = x.stride(), grad_out.stride(), grad_x.stride()
+        return cls(x.data_ptr(), grad_out.data_ptr(), weight.data_ptr(), grad_x.data_ptr(), grad_weight.data_ptr(), xs[0], xs[1],
+                   gs[0], gs[1], os[0], os[1], x.shape[1], 0)
 
 
 _i32p = C.POINTER(C.c_int32)
