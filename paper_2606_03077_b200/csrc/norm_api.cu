@@ -49,13 +49,13 @@ int lay_out(NormParams* p, bool wide, int v) {
   if (D % v != 0 || R % (half ? 2 * v : v) != 0) return 0;
   p->items = half ? R / (2 * v) + ((D - R) / v + 1) / 2 : (D / v + 1) / 2;
   if (p->items > 32) return 0;
-  for (p->lanes = 1; p->lanes < p->items; p->lanes *= 2) {}
+  for (p->lanes_shift = 0; 1 << p->lanes_shift < p->items; ++p->lanes_shift) {}
   return v;
 }
 
 // Steps of every kind and of a token: the rows that a warp holds at once, or one
 void count_steps(NormParams* p, bool by_lanes) {
-  const int rows = by_lanes ? 32 / p->lanes : 1;
+  const int rows = by_lanes ? 32 >> p->lanes_shift : 1;
   p->steps = 0;
   for (NormKind& k : p->kind) p->steps += k.steps = (k.n_heads + rows - 1) / rows;
 }

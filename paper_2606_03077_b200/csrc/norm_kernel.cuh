@@ -60,7 +60,7 @@ struct NormParams {
   float eps, inv_dim;
   int32_t head_dim, page_shift;
   int32_t steps;               // of a token, of all kinds
-  int32_t items, lanes;        // of a row; lanes: the power of two that holds them
+  int32_t items, lanes_shift;  // of a row, and the power of two of lanes that holds them
   libra_rope_t rope;
 };
 
@@ -132,10 +132,14 @@ struct Raw {
     } else {
 #pragma unroll
       for (int i = 0; i < kWords; ++i) {
-        T t[2];
-        *reinterpret_cast<uint32_t*>(t) = w[i];
-        f[2 * i] = rope::to_f32(t[0]);
-        f[2 * i + 1] = rope::to_f32(t[1]);
+        if constexpr (std::is_same<T, __half>::value) {
+          const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+          f[2 * i] = t.x;
+          f[2 * i + 1] = t.y;
+        } else {
+          f[2 * i] = __uint_as_float(w[i] << 16);
+          f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
       }
     }
   }
@@ -290,6 +294,26 @@ __device__ __forceinline__ void st_shared_zero(uint32_t at) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
 }
 
+// The steps of warp `me` of `warps`: a run of consecutive ones, step s of the launch being step s % steps of token s / steps.
+struct Run {
+  int32_t token, step, left;
+  __device__ __forceinline__ Run(int64_t n_tokens, int32_t steps, uint32_t warps, uint32_t me) {
+    const int64_t all = n_tokens * steps;
+    if (all <= 0x7fffffff) {   // a division of 64 bits takes a hundred instructions
+      const uint32_t run = (uint32_t(all) + warps - 1) / warps;
+      const int64_t begin = int64_t(me) * run;
+      left = int32_t(max(int64_t(0), min(int64_t(run), all - begin)));
+      token = left > 0 ? int32_t(uint32_t(begin) / uint32_t(steps)) : 0;
+      step = left > 0 ? int32_t(uint32_t(begin) - uint32_t(token) * uint32_t(steps)) : 0;
+    } else {
+      const int64_t run = (all + warps - 1) / warps, begin = me * run;
+      left = int32_t(max(int64_t(0), min(run, all - begin)));
+      token = left > 0 ? int32_t(begin / steps) : 0;
+      step = left > 0 ? int32_t(begin - int64_t(token) * steps) : 0;
+    }
+  }
+};
+
 // A warp's walk over rows: row u of the launch is row u % units of token u / units.
 struct Units {
   int64_t token;
@@ -331,16 +355,15 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
   for (int i = threadIdx.x; i < pairs; i += kNormThreads) turns[i] = p.rope.turns[i];
   if constexpr (kAppend) asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
-  const int item = lane & (p.lanes - 1), group = lane / p.lanes, groups = 32 / p.lanes;
+  const int lanes = 1 << p.lanes_shift, item = lane & (lanes - 1), group = lane >> p.lanes_shift, groups_shift = 5 - p.lanes_shift, groups = 1 << groups_shift;
   const bool on = item < p.items;
   const Item<V, kHalf> it(item, p.items, R);
   const Factors<V, kHalf> turn(factors[warp], R);
   const bool two = on && it.c1 < p.head_dim;
   int64_t n_tokens = p.n_tokens;
   if (kAppend && p.n_rows) n_tokens = max(int64_t(0), min(n_tokens, int64_t(*p.n_rows)));
-  const int64_t all = n_tokens * p.steps, warps = int64_t(gridDim.x) * kNormWarps, me = int64_t(blockIdx.x) * kNormWarps + warp;
-  const int64_t run = (all + warps - 1) / warps, begin = me * run;
-  int left = int(max(int64_t(0), min(run, all - begin)));
+  const Run run(n_tokens, p.steps, gridDim.x * kNormWarps, blockIdx.x * kNormWarps + warp);
+  int left = run.left;
   if (left == 0) return;
 
   struct Part {   // of the run: heads of one token and one kind
@@ -358,12 +381,11 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
       }
     }
     x.steps = min(most, p.kind[x.kind].steps - step);
-    x.head0 = step * groups + group;
-    x.rows = on ? min(x.steps, (p.kind[x.kind].n_heads - x.head0 + groups - 1) / groups) : 0;
+    x.head0 = (step << groups_shift) + group;
+    x.rows = on ? min(x.steps, (p.kind[x.kind].n_heads - x.head0 + groups - 1) >> groups_shift) : 0;
     return x;
   };
-  int64_t token = begin / p.steps;
-  int step = int(begin - token * p.steps);
+  int token = run.token, step = run.step;
 
   // ---- the copies, kNormAhead - 1 steps ahead.  Lanes and vectors that hold nothing are zero from the start.
   const uint32_t ring = dev::smem_u32(rings[warp]) + lane * 16;
@@ -371,7 +393,7 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
   for (int i = 0; i < 2 * kNormAhead; ++i) {
     if (i & 1 ? !two : !on) st_shared_zero(ring + i * 512);
   }
-  int64_t ask_token = token;
+  int ask_token = token;
   int ask_step = step, ask_left = left, ask_steps = 0, ask_rows = 0;
   const T* ask_src = nullptr;
   int64_t ask_hop = 0;
@@ -379,7 +401,7 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
     if (ask_steps == 0 && ask_left > 0) {
       const Part x = part_of(ask_step, ask_left);
       const NormKind& kind = p.kind[x.kind];
-      ask_src = static_cast<const T*>(kind.x) + ask_token * kind.x_token + x.head0 * kind.x_head + it.c0;
+      ask_src = static_cast<const T*>(kind.x) + int64_t(ask_token) * kind.x_token + x.head0 * kind.x_head + it.c0;
       ask_hop = groups * kind.x_head;
       ask_steps = x.steps;
       ask_rows = x.rows;
@@ -416,9 +438,9 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
     step += x.steps;
     const bool ends = step == p.steps;
     // the token after this one, while there is time
-    const int64_t after = ends && left > 0 ? token + 1 : token;
+    const int after = ends && left > 0 ? token + 1 : token;
     const int32_t next_pos = pairs > 0 ? __ldg(p.positions + after) : 0, next_slot = kAppend ? __ldg(p.slots + after) : 0;
-    int64_t at = pool ? slot_offset(p, slot) : token * kind.out_token;     // of the output, in elements
+    int64_t at = pool ? slot_offset(p, slot) : int64_t(token) * kind.out_token;     // of the output, in elements
     int rows = at >= 0 ? x.rows : 0;
     const int64_t out_head = pool ? p.stride_head : kind.out_head, hop = groups * out_head;
     at += x.head0 * out_head;
@@ -475,7 +497,7 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
             sum = fma2(a[k], a[k], sum);
             more = fma2(b[k], b[k], more);
           }
-          const float2 r = both(inverse_root(fmaf(group_sum((sum.x + more.x) + (sum.y + more.y), p.lanes), p.inv_dim, p.eps)));
+          const float2 r = both(inverse_root(fmaf(group_sum((sum.x + more.x) + (sum.y + more.y), lanes), p.inv_dim, p.eps)));
 #pragma unroll
           for (int k = 0; k < V / 2; ++k) {
             a[k] = mul2(a[k], r);
@@ -535,7 +557,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
   const int R = p.rope.rotary_dim, pairs = R / 2;
   for (int i = threadIdx.x; i < pairs; i += kThreads) turns[i] = p.rope.turns[i];
   __syncthreads();
-  const int item = lane & (p.lanes - 1), group = lane / p.lanes, groups = 32 / p.lanes;
+  const int lanes = 1 << p.lanes_shift, item = lane & (lanes - 1), group = lane >> p.lanes_shift, groups_shift = 5 - p.lanes_shift, groups = 1 << groups_shift;
   const bool on = item < p.items;
   const Item<V, kHalf> it(item, p.items, R);
   const Factors<V, kHalf> turn(factors[warp], R);
@@ -543,11 +565,8 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
   float2 wa[V / 2], wb[V / 2], acca[2][V / 2], accb[2][V / 2];   // the kind's weights; sums of both
 #pragma unroll
   for (int k = 0; k < V / 2; ++k) acca[0][k] = accb[0][k] = acca[1][k] = accb[1][k] = both(0.f);
-  const int64_t all = p.n_tokens * p.steps, warps = int64_t(gridDim.x) * kWarps, me = int64_t(blockIdx.x) * kWarps + warp;
-  const int64_t run = (all + warps - 1) / warps, begin = me * run;
-  int left = int(max(int64_t(0), min(run, all - begin)));
-  int64_t token = left > 0 ? begin / p.steps : 0;
-  int step = left > 0 ? int(begin - token * p.steps) : 0;
+  const Run run(p.n_tokens, p.steps, gridDim.x * kWarps, blockIdx.x * kWarps + warp);
+  int token = run.token, step = run.step, left = run.left;
 
   struct Part {   // of the run: heads of one token and one kind
     int kind, head0, steps, rows;   // this lane's first head, steps, rows of this lane's group
@@ -557,8 +576,8 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
     x.kind = at >= p.kind[0].steps ? 1 : 0;
     if (x.kind) at -= p.kind[0].steps;
     x.steps = min(most, p.kind[x.kind].steps - at);
-    x.head0 = at * groups + group;
-    x.rows = on ? min(x.steps, (p.kind[x.kind].n_heads - x.head0 + groups - 1) / groups) : 0;
+    x.head0 = (at << groups_shift) + group;
+    x.rows = on ? min(x.steps, (p.kind[x.kind].n_heads - x.head0 + groups - 1) >> groups_shift) : 0;
     return x;
   };
   const uint32_t ring = dev::smem_u32(rings) + warp * kRing + lane * 16;
@@ -566,7 +585,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
   for (int i = 0; i < 4 * kNormGradAhead; ++i) {
     if (i & 1 ? !two : !on) st_shared_zero(ring + i * 512);
   }
-  int64_t ask_token = token;
+  int ask_token = token;
   int ask_step = step, ask_left = left, ask_steps = 0, ask_rows = 0;
   const T *ask_src = nullptr, *ask_grad = nullptr;
   int64_t src_hop = 0, grad_hop = 0;
@@ -574,8 +593,8 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
     if (ask_steps == 0) {
       const Part x = part_of(ask_step, ask_left);
       const NormKind& kind = p.kind[x.kind];
-      ask_src = static_cast<const T*>(kind.x) + ask_token * kind.x_token + x.head0 * kind.x_head + it.c0;
-      ask_grad = static_cast<const T*>(kind.grad) + ask_token * kind.grad_token + x.head0 * kind.grad_head + it.c0;
+      ask_src = static_cast<const T*>(kind.x) + int64_t(ask_token) * kind.x_token + x.head0 * kind.x_head + it.c0;
+      ask_grad = static_cast<const T*>(kind.grad) + int64_t(ask_token) * kind.grad_token + x.head0 * kind.grad_head + it.c0;
       src_hop = groups * kind.x_head;
       grad_hop = groups * kind.grad_head;
       ask_steps = x.steps;
@@ -616,7 +635,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
     step += x.steps;
     const bool ends = step == p.steps;
     const int32_t next_pos = pairs > 0 ? __ldg(p.positions + (ends && left > 0 ? token + 1 : token)) : 0;
-    T* out = static_cast<T*>(kind.out) + token * kind.out_token + x.head0 * kind.out_head;
+    T* out = static_cast<T*>(kind.out) + int64_t(token) * kind.out_token + x.head0 * kind.out_head;
     const int64_t out_hop = groups * kind.out_head;
     {
       float w0[V], w1[V];
@@ -671,7 +690,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
         dots = fma2(mul2(gb[k], xb[k]), wb[k], dots);
       }
       float sum[2] = {(square.x + more.x) + (square.y + more.y), (dot.x + dots.x) + (dot.y + dots.y)};
-      group_sums(sum, p.lanes);
+      group_sums(sum, lanes);
       const float r = inverse_root(fmaf(sum[0], p.inv_dim, p.eps));
       const float2 r2 = both(r), m2 = both(-(sum[1] * p.inv_dim * r * r * r));   // dx = r w g - x r^3 mean(w g x)
       if (j < x.rows) {
@@ -717,7 +736,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
     from_pairs<V, kHalf>(acca[kd], accb[kd], acc0, acc1);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      for (int off = p.lanes; off < 32; off <<= 1) {
+      for (int off = lanes; off < 32; off <<= 1) {
         acc0[k] += __shfl_xor_sync(0xffffffffu, acc0[k], off);
         acc1[k] += __shfl_xor_sync(0xffffffffu, acc1[k], off);
       }
