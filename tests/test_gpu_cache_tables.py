@@ -246,6 +246,53 @@ def test_recorded_and_replayed(lib):
     t.h.close()
 
 
+def test_recorded_with_as_many_sequences_as_there_can_be(lib):
+    """The prefix sums of 4096 sequences need more shared memory than the default; the first call is within the recording."""
+    import torch
+    rng = np.random.default_rng(4)
+    lens = rng.integers(0, 40, 4096)
+    t = Tables(lib, lens, 6, spare=4096 * 2)
+    new = rng.integers(0, 30, 4096)
+    t.change.copy_(torch.tensor(new.astype(np.int32)))
+    t.rows_for(int(new.sum()))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        t.extend(None)
+    g.replay()
+    torch.cuda.synchronize()
+    assert int(t.err) == 0
+    t.check_rows(*t.model_extend(new))
+    t.check_state()
+    del g
+    t.h.close()
+
+
+def test_a_table_row_of_2_to_the_31_tokens(lib):
+    """Lengths next to the largest one; a sequence of 2^31 - 1 tokens cannot grow."""
+    import torch
+    h = lib.Handle(8, 2, 64, 2 ** 25 - 1, 2, 2 ** 25, page_size=64)   # one page more would be refused
+    table = torch.zeros((2, 2 ** 25), dtype=torch.int32, device="cuda")
+    last = 2 ** 31 - 1
+    lens = torch.tensor([last - 65, last], dtype=torch.int32, device="cuda")
+    free, count = torch.arange(100, 110, dtype=torch.int32, device="cuda").repeat(2 ** 22)[:2 ** 25].contiguous(), torch.tensor([10], dtype=torch.int32, device="cuda")
+    off, pos, slots, err = (torch.full((n,), CANARY, dtype=torch.int32, device="cuda") for n in (3, 70, 70, 1))
+    err.zero_()
+
+    def extend(new):
+        change = torch.tensor(new, dtype=torch.int32, device="cuda")
+        h.cache_extend(change.data_ptr(), lens.data_ptr(), table.data_ptr(), 2, free.data_ptr(), count.data_ptr(), off.data_ptr(), pos.data_ptr(),
+                       slots.data_ptr(), 70, err.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        return int(err)
+
+    assert extend([65, 1]) == lib.ERR_PLAN_OVERFLOW and off.tolist() == [0, 0, 0] and lens.tolist() == [last - 65, last]
+    err.zero_()
+    assert extend([65, 0]) == 0 and lens.tolist() == [last, last] and int(count) == 9
+    assert pos[:65].tolist() == list(range(last - 65, last)) and int(table[0, 2 ** 25 - 1]) == 109
+    old, new = [0 * 64 + i for i in range(62, 64)], [109 * 64 + i for i in range(63)]
+    assert slots[:65].tolist() == old + new
+    h.close()
+
+
 def test_refused_by_the_host(lib):
     import torch
     t = Tables(lib, [5, 16], 6, spare=3)

@@ -271,6 +271,127 @@ def test_many_rows_the_same_bits_and_recorded(lib, dim):
     del graphs
 
 
+def torch_forward(x, w, pos, rotary, layout, eps=EPS):
+    """The forward map in float64 on the device, and the bound before the last rounding."""
+    import torch
+    x, w = x.double(), w.double()
+    r = (x.square().mean(-1, keepdim=True) + float(np.float32(eps))).rsqrt()
+    n, D = x * r * w, x.shape[-1]
+    theta = torch.tensor([10000.0 ** (-2.0 * i / rotary) for i in range(rotary // 2)], dtype=torch.float64, device=x.device)
+    a = pos.double()[:, None, None] * theta
+    h = rotary // 2
+    u, v = (n[..., :h], n[..., h:rotary]) if layout == K.HALF else (n[..., 0:rotary:2], n[..., 1:rotary:2])
+    yu, yv, both = u * a.cos() - v * a.sin(), u * a.sin() + v * a.cos(), u.abs() + v.abs()
+    y, e = n.clone(), (D * U / 2 + 4 * U) * n.abs()
+    for at, val in ((0, yu), (1, yv)):
+        sl = slice(at * h, at * h + h) if layout == K.HALF else slice(at, rotary, 2)
+        # float64 angles of up to 2^13 radians are right to 2^-39
+        y[..., sl], e[..., sl] = val, (2.0 ** -21 + D * U / 2 + 4 * U + 2.0 ** -38) * both
+    return y, e
+
+
+@pytest.mark.parametrize("layout", [K.HALF, K.INTERLEAVED])
+@pytest.mark.parametrize("dim,rotary", [(128, 128), (80, 40), (256, 64), (48, 12)])
+@pytest.mark.parametrize("hq,hk", [(24, 5), (7, 7), (33, 0)])
+def test_runs_that_begin_anywhere(lib, hq, hk, dim, rotary, layout):
+    """More steps than warps, so that the warps' runs begin and end within a token, a kind and a group of heads."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(dim + hq)
+    tokens = 2503
+    draw = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+    rope, pos = rope_of(lib, rotary, layout), torch.randint(0, 8000, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    xs, ws = [draw(tokens, h, dim) for h in (hq, hk) if h], [draw(dim) for _ in range(2)]
+    outs = [torch.full_like(x, float("nan")) for x in xs]
+    rows = [lib.NormRows.of(x, w, o) for x, w, o in zip(xs, ws, outs)] + [None]
+    lib.libra_norm_rope_apply(0, rope, rows[0], rows[1], lib.ROPE_BF16, pos.data_ptr(), tokens, dim, EPS, stream())
+    for x, w, o in zip(xs, ws, outs):
+        ref, e = torch_forward(x, w, pos, rotary, layout)
+        assert bool(((o.double() - ref).abs() <= e + HALF_STEP["bf16"] * (ref.abs() + e) + TINY["bf16"]).all())
+
+
+@pytest.mark.parametrize("order", ["HND", "NHD"])
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+def test_append_of_many_rows(lib, kv, order):
+    import torch
+    rows, hq, hkv, dim, page = 3001, 40, 8, 128, 32
+    a = Append(lib, rows, hq, hkv, dim, page, order, kv, seed=7, dead={17: -1})
+    a.n[0] = rows - 3
+    a.pos %= 8000
+    a.dpos.copy_(torch.from_numpy(a.pos))
+    a.call(rope_of(lib, dim))
+    n = rows - 3
+    ref, e = torch_forward(a.q[:n], a.w[0], a.dpos[:n], dim, K.HALF)
+    assert bool(((a.out[:n].double() - ref).abs() <= e + HALF_STEP["bf16"] * (ref.abs() + e) + TINY["bf16"]).all())
+    assert bool(torch.isnan(a.out[n:]).all()) and int(a.err) == 0
+    ky, ke = torch_forward(a.kn[:n], a.w[1], a.dpos[:n], dim, K.HALF)
+    live = torch.from_numpy(a.slots[:n] >= 0).cuda()
+    s = a.dslots[:n].long()[live]
+    for pool, before, y, e, scale in ((a.k, a.k0, ky, ke, a.scales[0]), (a.v, a.v0, a.vn[:n].double(), torch.zeros_like(ky), a.scales[1])):
+        now, was = (x if order == "NHD" else x.transpose(1, 2) for x in (pool, before.clone()))
+        got = now[s // page, s % page]
+        was[s // page, s % page] = got
+        assert torch.equal(now, was)      # every other slot as it was
+        if kv == "bf16":
+            got, half, least = got.view(torch.bfloat16).double(), 2.0 ** -8, 2.0 ** -134
+        else:
+            # the float32 product with the rounded reciprocal: 2^-22; half a step of E4M3, or of its smallest numbers
+            got, half, least = got.view(torch.float8_e4m3fn).double() * scale, 2.0 ** -4 + 2.0 ** -21, 2.0 ** -10 * scale
+            y = y.clamp(-448 * scale, 448 * scale)
+        y, e = y[live], e[live]
+        assert bool(((got - y).abs() <= e + half * (y.abs() + e) + least).all())
+    a.h.close()
+
+
+def test_rows_far_apart_and_more_steps_than_31_bits_count(lib):
+    """Tokens 2.4 GB from one another; and 1.1e9 tokens of one broadcast row, of q and of k."""
+    import torch
+    dim, far = 128, 1_200_000_000
+    wide = torch.zeros(2 * far + 4 * dim, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(wide, (3, 2, dim), (far, 2 * dim, 1), 0)
+    x.copy_(torch.randn((3, 2, dim), device="cuda"))
+    w, pos = torch.ones(dim, dtype=torch.bfloat16, device="cuda"), torch.tensor([5, 6, 7], dtype=torch.int32, device="cuda")
+    near, dense = x.contiguous(), torch.empty((3, 2, dim), dtype=torch.bfloat16, device="cuda")
+    rope = rope_of(lib, dim)
+    lib.libra_norm_rope_apply(0, rope, lib.NormRows.of(near, w, dense), None, lib.ROPE_BF16, pos.data_ptr(), 3, dim, EPS, stream())
+    lib.libra_norm_rope_apply(0, rope, lib.NormRows.of(x, w, x), None, lib.ROPE_BF16, pos.data_ptr(), 3, dim, EPS, stream())
+    assert torch.equal(x, dense)
+    del wide, x
+    tokens, dim = 1_100_000_000, 8
+    row = torch.randn((1, 1, dim), device="cuda").to(torch.bfloat16)
+    w, outs = torch.ones(dim, dtype=torch.bfloat16, device="cuda"), [torch.zeros((tokens, 1, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    q, k = (lib.NormRows.of(row.expand(tokens, 1, dim), w, o) for o in outs)
+    assert q.x_stride_token == 0
+    lib.libra_norm_rope_apply(0, None, q, k, lib.ROPE_BF16, 0, tokens, dim, EPS, stream())
+    for o in outs:
+        words = o.view(torch.int64).view(-1, 2)
+        for at in range(0, tokens, 1 << 27):
+            part = words[at:at + (1 << 27)]
+            assert bool((part == words[0]).all())
+    assert float(outs[0][0].abs().max()) > 0 and torch.equal(outs[0][0], outs[1][0])
+
+
+def test_recorded_where_the_kernel_needs_more_shared_memory_than_the_default(lib):
+    """Heads of 1022 channels in float32 through shared memory, gradient of q and k, first call within the recording."""
+    import torch
+    rng = np.random.default_rng(2)
+    x, g = ([torch.from_numpy(rng.standard_normal((5, h, 1022)).astype(np.float32)).cuda() for h in (2, 1)] for _ in range(2))
+    w = [torch.from_numpy(rng.standard_normal(1022).astype(np.float32)).cuda() for _ in range(2)]
+    o, gw = [torch.empty_like(t) for t in x], [torch.empty_like(t) for t in w]
+    pos = torch.arange(5, dtype=torch.int32, device="cuda")
+    ws = torch.empty(lib.libra_norm_rope_workspace_size(0, 1022), dtype=torch.uint8, device="cuda")
+    q, k = (lib.NormGrads.of(*a) for a in zip(x, g, w, o, gw))
+    rope = rope_of(lib, 254)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lib.libra_norm_rope_gradient(0, rope, q, k, lib.ROPE_F32, pos.data_ptr(), 5, 1022, EPS, ws.data_ptr(), ws.numel(), stream())
+    graph.replay()
+    angles = K.rope_angles(pos.cpu().numpy(), K.rope_turns(254, 10000.0))
+    for i in range(2):
+        dx, dw, e, ew = gradient(f64(x[i]), f64(g[i]), f64(w[i]), angles, K.HALF, 1.0, float(np.float32(EPS)))
+        assert np.all(np.abs(f64(o[i]) - dx) <= rounded(dx, e, "f32")) and np.all(np.abs(f64(gw[i]) - dw) <= ew + U * np.abs(dw))
+    del graph
+
+
 def test_no_tokens(lib):
     import torch
     x, w = torch.zeros((1, 2, 64), device="cuda"), torch.ones(64, device="cuda")

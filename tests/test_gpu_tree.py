@@ -178,6 +178,18 @@ def test_rows_that_see_nothing(lib):
         c.check(); c.h.close()
 
 
+def test_cut_ranges_that_hold_nothing_for_a_row(lib):
+    """A tree of 700 tokens and nothing cached, its range cut: rows that see nothing in some of the parts, and in none."""
+    rng = np.random.default_rng(11)
+    n = 700
+    sees = rng.random((n, n)) < 0.004
+    sees[::7] = False
+    assert len(lib.libra_chunk_plan_host(148, 4, 1, [n], [n])["merges"]) > 0
+    for dim in (64, 128):
+        c = TreeCase(lib, [n], [n], 4, 1, dim, sees=[sees], seed=dim)
+        c.run()
+
+
 @pytest.mark.parametrize("kv", ["bf16", "e4m3"])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_a_chain_is_a_chunk(lib, dim, kv):
