@@ -164,8 +164,8 @@ int libra_norm_rope_apply(int32_t device, const libra_rope_t* rope, const libra_
                                               : apply_fn<float, 4>(vec, wide, half);
   const int warps = by_lanes ? libra::kNormWarps : libra::kNormAnyWarps;
   const unsigned grid = blocks_for(n_tokens * p.steps, warps, int64_t(n_sm) * (by_lanes ? libra::kNormBlocks : 16));
-  fn<<<grid, warps * 32, by_lanes ? 0 : size_t(warps) * head_dim * sizeof(float), static_cast<cudaStream_t>(stream)>>>(p);
-  const cudaError_t e = cudaGetLastError();
+  const size_t smem = by_lanes ? 0 : size_t(warps) * head_dim * sizeof(float);
+  const cudaError_t e = libra::launch(true, 1, fn, dim3(grid), unsigned(warps * 32), smem, static_cast<cudaStream_t>(stream), p);
   return e == cudaSuccess ? LIBRA_OK : fail_cuda(nullptr, e);
 }
 
@@ -248,8 +248,7 @@ int libra_norm_rope_gradient(int32_t device, const libra_rope_t* rope, const lib
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
     if (e != cudaSuccess) return fail_cuda(nullptr, e);
   }
-  fn<<<blocks, warps * 32, smem, st>>>(p);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = libra::launch(true, 1, fn, dim3(blocks), unsigned(warps * 32), smem, st, p);
   if (e != cudaSuccess) return fail_cuda(nullptr, e);
   s.partial = p.partial;
   s.head_dim = head_dim;

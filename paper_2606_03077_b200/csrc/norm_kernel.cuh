@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int R = p.rope.rotary_dim, pairs = R / 2;
   for (int i = threadIdx.x; i < pairs; i += kNormThreads) turns[i] = p.rope.turns[i];
-  if constexpr (kAppend) asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
   const int lanes = 1 << p.lanes_shift, item = lane & (lanes - 1), group = lane >> p.lanes_shift, groups_shift = 5 - p.lanes_shift, groups = 1 << groups_shift;
   const bool on = item < p.items;
@@ -556,6 +556,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int R = p.rope.rotary_dim, pairs = R / 2;
   for (int i = threadIdx.x; i < pairs; i += kThreads) turns[i] = p.rope.turns[i];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
   const int lanes = 1 << p.lanes_shift, item = lane & (lanes - 1), group = lane >> p.lanes_shift, groups_shift = 5 - p.lanes_shift, groups = 1 << groups_shift;
   const bool on = item < p.items;
@@ -796,7 +797,7 @@ __global__ void __launch_bounds__(kNormAnyThreads) norm_rope_any_kernel(const __
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = p.head_dim;
   const int R = p.rope.rotary_dim, pairs = R / 2;
   for (int i = threadIdx.x; i < pairs; i += kNormAnyThreads) turns[i] = p.rope.turns[i];
-  if constexpr (kAppend) asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
   float* const row = rows + warp * D;
   float2* const cs = factors[warp];
@@ -880,6 +881,7 @@ __global__ void __launch_bounds__(kNormAnyThreads) norm_rope_gradient_any_kernel
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = p.head_dim;
   const int R = p.rope.rotary_dim, pairs = R / 2;
   for (int i = threadIdx.x; i < pairs; i += kNormAnyThreads) turns[i] = p.rope.turns[i];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int kinds = p.kind[1].n_heads > 0 ? 2 : 1, channels = kinds * D;
   float* const xs = rows + (kinds * kNormAnyWarps + warp) * D;
   float* const gs = xs + kNormAnyWarps * D;
