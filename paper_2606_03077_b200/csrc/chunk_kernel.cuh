@@ -26,8 +26,16 @@
 // 64 / 8 heads: 1.44 ms = 1333 TFLOP/s in short runs, 80 % of a plain bf16 matrix product's burst rate (1663); the products and
 // copies alone take 1.17 ms, without the exponentials it is 1.39.  In runs of a tenth of a second and more the power cap holds the
 // clock at 1.62 GHz: 1.66 ms = 1160 TFLOP/s.  Three tokens on eight trajectories of 32K: 187 us = 5.7 TB/s of the cache (165 us
-// when the same inputs are read again).  Over an E4M3 cache the
-// conversion adds 96 KB of shared-memory traffic a step: 10 - 15 % slower than bf16 where arithmetic bounds.
+// when the same inputs are read again).
+//
+// Over an E4M3 cache the conversion adds 96 KB of shared-memory traffic a step (a step of one row tile: 224 KB in all, 0.94 us at 128 bytes
+// a cycle).  Steps of 144 blocks, 8K tokens each: 1.83 us for two row tiles (bf16: 2.04), 1.04 us for 20 - 60 rows, which are 3.9 TB/s of
+// codes (bf16: 1.36 us, 6.3 TB/s).  What starts and ends a block takes 8 - 12 us.
+//
+// Trees of drafted tokens (kTree): a row sees all cached tokens and, of the new ones, those that its bits in the mask name.  Only the
+// steps that reach the new tokens, one or two as a rule, put the row's words together from two neighbouring ones and select by
+// them; the rest of the build is the chunks'.  16 drafted tokens on eight trajectories of 32K, 64 / 8 heads: 169 us = 6.3 TB/s in
+// short runs, 198 where the power cap holds the clock at 1.4 - 1.75 GHz.
 //
 // Copies: one tiled TMA load per page (16, 32 or 64 tokens) and 64 channels, 128-byte swizzle, into a ring of tiles.  Pages
 // past the range are not read; what their rows of V hold is overwritten with zeros (0 x NaN would reach the result), scores

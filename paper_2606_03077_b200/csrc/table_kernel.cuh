@@ -14,7 +14,8 @@
 // between the blocks.  All checks are made on the sums before anything is written.  seq_lens and the
 // count change in place: the first block writes them once all have read them (cluster barrier).
 //
-// What bounds it: latency.
+// What bounds it: latency; in long batches the instructions of eight multiprocessors.  A step of 64 sequences, extend and trim: 6 us
+// together; 256 sequences with 115K new tokens: 13 us together (a row a thread 18, four rows 14.5).
 #pragma once
 #include <cuda_runtime.h>
 
