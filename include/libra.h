@@ -561,7 +561,7 @@ int libra_chunk_plan_host(int32_t n_sm, int32_t num_q_heads, int32_t num_kv_head
  * most max_tokens new tokens together (256-byte aligned; not the workspace of libra_plan). */
 int libra_chunk_workspace_size(libra_handle_t handle, int64_t max_tokens, size_t* bytes);
 
-/* Plan a batch for libra_chunk_attn from host lengths (int32[batch] each) and enqueue the plan's copy into the workspace on
+/* Plan a batch for libra_chunk_attn (and libra_tree_attn) from host lengths (int32[batch] each) and enqueue the plan's copy into the workspace on
  * `stream`.  One plan serves any number of libra_chunk_attn calls on the same lengths (the layers of a model), one after another:
  * on one stream, or on streams that events put in order, the plan's first, since cut ranges leave their partial results in the
  * workspace.  The call takes 12 us of the host, and up to 115 us where it tries cuts (up to 26 simulated launches).  Independent of
@@ -710,14 +710,15 @@ int libra_tree_mask(libra_handle_t handle, const int32_t* parents, const int32_t
  * the mask has bit j set (bits past i are ignored, and i itself is seen only where its bit is set).  A row that sees nothing gets
  * zeros and lse -inf.  The plan is libra_chunk_plan's for the same lengths; mask: uint32[rows, mask_ld], 4-byte aligned, mask_ld * 32 >=
  * the most new tokens of a sequence (INVALID_ARGUMENT otherwise; here mask_ld has no upper limit).  Everything else as
- * libra_chunk_attn, with one difference: a V that is not finite in a slot that a row does not see may reach that row. */
+ * libra_chunk_attn: what a row does not see never counts, but for a V that is not finite, which may reach every new row of its
+ * sequence and KV head. */
 int libra_tree_attn(libra_handle_t handle, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
                     const int32_t* block_table, const uint32_t* mask, int32_t mask_ld, void* out, float* lse, void* error_word_dev,
                     void* stream);
 
 /* After the verification: kept[b * kept_ld + i], i < n_kept[b], are the places of the accepted tokens among sequence b's new ones, in
  * ascending order (a path's are).  Their rows of K and V move to the slots n_cached + i, in the pools given (one layer's); other slots
- * stay.  new_lens[b] (or NULL; not the same array as seq_lens) = n_cached + n_kept[b], which is what libra_cache_trim takes.  Rows that
+ * stay.  new_lens[b] (or NULL; overlapping no input) = n_cached + n_kept[b], which is what libra_cache_trim takes.  Rows that
  * do not ascend, or more of them than there are new tokens or than kept_ld, set LIBRA_ERR_BAD_TREE, a length that cannot be
  * LIBRA_ERR_BAD_LENGTH, one past the end of a block-table row LIBRA_ERR_PLAN_OVERFLOW: then nothing of that sequence moves and
  * new_lens[b] = seq_lens[b].  A page id outside the pool sets LIBRA_ERR_BAD_PAGE_ID and the row is not moved.

@@ -15,6 +15,9 @@
 // pairs an instruction.  Rows that this does not fit (rotated parts or heads that the items do not divide, addresses off a 16-byte boundary, heads of
 // more items than a warp has lanes) are held whole in shared memory, one a warp, in the kernels at the end.
 //
+// The kernels may be launched while the one before still runs and wait for it first (programmatic dependent launch).  What that one may
+// have written - positions, slots, weights too - is therefore read by ordinary loads: the read-only path's could be moved ahead of the wait.
+//
 // dw is summed in registers along a warp's run, then over the warps and the blocks in a fixed order: the same bits every time.
 //
 // Measured (device, changing inputs): 8191 tokens of 40 + 8 heads of 128, fp16, half of each rotated, 36 us = 5.6 TB/s; gradient of 16384
@@ -118,9 +121,9 @@ template <typename T, int V>
 struct Raw {
   static constexpr int kWords = V * int(sizeof(T)) / 4;
   uint32_t w[kWords];
-  __device__ __forceinline__ void load(const T* p) {   // by the read-only path
-    if constexpr (kWords == 4) set(__ldg(reinterpret_cast<const uint4*>(p)));
-    else set(__ldg(reinterpret_cast<const uint2*>(p)));
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kWords == 4) set(*reinterpret_cast<const uint4*>(p));
+    else set(*reinterpret_cast<const uint2*>(p));
   }
   __device__ __forceinline__ void load_shared(uint32_t at) {
     if constexpr (kWords == 4) {
@@ -434,7 +437,7 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
     copies_commit();
   }
 
-  int32_t pos = pairs > 0 ? __ldg(p.positions + token) : 0, slot = kAppend ? __ldg(p.slots + token) : 0;
+  int32_t pos = pairs > 0 ? p.positions[token] : 0, slot = kAppend ? p.slots[token] : 0;
   bool new_token = true;
   uint32_t place = 0;
 #pragma unroll 1
@@ -447,7 +450,7 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
     const bool ends = step == p.steps;
     // the token after this one, while there is time
     const int after = ends && left > 0 ? token + 1 : token;
-    const int32_t next_pos = pairs > 0 ? __ldg(p.positions + after) : 0, next_slot = kAppend ? __ldg(p.slots + after) : 0;
+    const int32_t next_pos = pairs > 0 ? p.positions[after] : 0, next_slot = kAppend ? p.slots[after] : 0;
     int64_t at = pool ? slot_offset(p, slot) : int64_t(token) * kind.out_token;     // of the output, in elements
     int rows = at >= 0 ? x.rows : 0;
     const int64_t out_head = pool ? p.stride_head : kind.out_head, hop = groups * out_head;
@@ -633,7 +636,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
     if (i < left) ask(i * kStep);
     copies_commit();
   }
-  int32_t pos = pairs > 0 && left > 0 ? __ldg(p.positions + token) : 0;
+  int32_t pos = pairs > 0 && left > 0 ? p.positions[token] : 0;
   bool new_token = true;
   uint32_t place = 0;
 #pragma unroll 1
@@ -643,7 +646,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
     left -= x.steps;
     step += x.steps;
     const bool ends = step == p.steps;
-    const int32_t next_pos = pairs > 0 ? __ldg(p.positions + (ends && left > 0 ? token + 1 : token)) : 0;
+    const int32_t next_pos = pairs > 0 ? p.positions[ends && left > 0 ? token + 1 : token] : 0;
     T* out = static_cast<T*>(kind.out) + int64_t(token) * kind.out_token + x.head0 * kind.out_head;
     const int64_t out_hop = groups * kind.out_head;
     {
@@ -827,11 +830,11 @@ __global__ void __launch_bounds__(kNormAnyThreads) norm_rope_any_kernel(const __
     const NormKind& kind = p.kind[kd];
     const T* const src = static_cast<const T*>(kind.x) + u.token * kind.x_token + head * kind.x_head;
     const bool pool = kAppend && kd > 0;
-    const int64_t at = pool ? slot_offset(p, __ldg(p.slots + u.token)) : u.token * kind.out_token;
+    const int64_t at = pool ? slot_offset(p, p.slots[u.token]) : u.token * kind.out_token;
     const bool normed = kind.weight != nullptr, turned = !(kAppend && kd == 2) && R > 0;
     __syncwarp();   // the row before has been read
     if (turned) {
-      const int32_t pos = __ldg(p.positions + u.token);
+      const int32_t pos = p.positions[u.token];
       for (int i = lane; i < pairs; i += 32) cs[i] = rope::cos_sin(pos, turns[i], p.rope.magnitude);
     }
     float sum = 0.f;
@@ -908,7 +911,7 @@ __global__ void __launch_bounds__(kNormAnyThreads) norm_rope_gradient_any_kernel
     const T* const grad = static_cast<const T*>(kind.grad) + u.token * kind.grad_token + head * kind.grad_head;
     __syncwarp();
     if (R > 0) {
-      const int32_t pos = __ldg(p.positions + u.token);
+      const int32_t pos = p.positions[u.token];
       for (int i = lane; i < pairs; i += 32) cs[i] = rope::cos_sin(pos, turns[i], p.rope.magnitude);
     }
     float square = 0.f;
