@@ -704,25 +704,30 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
       float sum[2] = {(square.x + more.x) + (square.y + more.y), (dot.x + dots.x) + (dot.y + dots.y)};
       group_sums(sum, lanes);
       const float r = inverse_root(fmaf(sum[0], p.inv_dim, p.eps));
-      const float2 r2 = both(r), m2 = both(-(sum[1] * p.inv_dim * r * r * r));   // dx = r w g - x r^3 mean(w g x)
+      const float2 r2 = both(r), mean2 = both(-(sum[1] * p.inv_dim * r));   // minus the mean of w g x r
       if (j < x.rows) {
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k) {
+          xa[k] = mul2(xa[k], r2);
+          xb[k] = mul2(xb[k], r2);
+        }
         if (x.kind == 0) {
 #pragma unroll
           for (int k = 0; k < V / 2; ++k) {
-            acca[0][k] = fma2(mul2(ga[k], xa[k]), r2, acca[0][k]);
-            accb[0][k] = fma2(mul2(gb[k], xb[k]), r2, accb[0][k]);
+            acca[0][k] = fma2(ga[k], xa[k], acca[0][k]);
+            accb[0][k] = fma2(gb[k], xb[k], accb[0][k]);
           }
         } else {
 #pragma unroll
           for (int k = 0; k < V / 2; ++k) {
-            acca[1][k] = fma2(mul2(ga[k], xa[k]), r2, acca[1][k]);
-            accb[1][k] = fma2(mul2(gb[k], xb[k]), r2, accb[1][k]);
+            acca[1][k] = fma2(ga[k], xa[k], acca[1][k]);
+            accb[1][k] = fma2(gb[k], xb[k], accb[1][k]);
           }
         }
 #pragma unroll
         for (int k = 0; k < V / 2; ++k) {
-          ga[k] = fma2(xa[k], m2, mul2(mul2(ga[k], wa[k]), r2));
-          gb[k] = fma2(xb[k], m2, mul2(mul2(gb[k], wb[k]), r2));
+          ga[k] = mul2(fma2(xa[k], mean2, mul2(ga[k], wa[k])), r2);
+          gb[k] = mul2(fma2(xb[k], mean2, mul2(gb[k], wb[k])), r2);
         }
         from_pairs<V, kHalf>(ga, gb, v0, v1);
         Raw<T, V>(v0).store(out + it.c0);

@@ -593,3 +593,24 @@ def test_append_refused(lib):
         a.h.norm_rope_append(*good)
     assert e.value.status == lib.INVALID_ARGUMENT
     a.h.close()
+
+
+@pytest.mark.parametrize("dim", [128, 24])
+def test_small_rows_and_a_small_epsilon(lib, dim):
+    """Rows far below the square root of epsilon, and an epsilon of 2^-100: r is up to 2^50, what is returned is no more than that."""
+    import torch
+    rng = np.random.default_rng(dim)
+    x = torch.from_numpy((rng.standard_normal((6, 4, dim)) * np.array([1, 2.0 ** -30, 2.0 ** -52, 2.0 ** -60, 0, 2.0 ** 40])[:, None, None]).astype(np.float32)).cuda()
+    g, w = (torch.from_numpy(rng.standard_normal(s).astype(np.float32)).cuda() for s in ((6, 4, dim), (dim,)))
+    pos, rope = torch.arange(6, dtype=torch.int32, device="cuda"), rope_of(lib, dim)
+    out, gx, gw = torch.empty_like(x), torch.empty_like(x), torch.empty_like(w)
+    ws = torch.empty(lib.libra_norm_rope_workspace_size(0, dim), dtype=torch.uint8, device="cuda")
+    angles = K.rope_angles(np.arange(6), K.rope_turns(dim, 10000.0))
+    for eps in (1e-6, 2.0 ** -100):
+        lib.libra_norm_rope_apply(0, rope, lib.NormRows.of(x, w, out), None, lib.ROPE_F32, pos.data_ptr(), 6, dim, eps, stream())
+        lib.libra_norm_rope_gradient(0, rope, lib.NormGrads.of(x, g, w, gx, gw), None, lib.ROPE_F32, pos.data_ptr(), 6, dim, eps, ws.data_ptr(), ws.numel(), stream())
+        e64 = float(np.float32(eps))
+        ref, e = forward(f64(x), f64(w), angles, K.HALF, 1.0, e64)
+        assert np.all(np.abs(f64(out) - ref) <= rounded(ref, e, "f32"))
+        dx, dw, e, ew = gradient(f64(x), f64(g), f64(w), angles, K.HALF, 1.0, e64)
+        assert np.all(np.abs(f64(gx) - dx) <= rounded(dx, e, "f32")) and np.all(np.abs(f64(gw) - dw) <= ew + U * np.abs(dw))
