@@ -48,7 +48,7 @@ int launch_table(libra_handle_t h, void (*fn)(libra::TableParams), const libra::
   if (smem > 40 * 1024) {   // beside the static part
     LIBRA_CUDA_TRY(h, cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
   }
-  int64_t threads = (p.batch + libra::kTablePerThread - 1) / libra::kTablePerThread;
+  int64_t threads = std::max(1, (p.batch + libra::kTablePerThread - 1) / libra::kTablePerThread);
   threads = std::max<int64_t>(threads, std::min<int64_t>(work, libra::kTableMaxThreads));
   threads = std::min<int64_t>((threads + 31) / 32 * 32, libra::kTableMaxThreads);
   unsigned blocks = 1;

@@ -182,6 +182,20 @@ def test_no_sequences(lib):
     t.h.close()
 
 
+def test_no_sequences_and_no_rows(lib):
+    t = Tables(lib, [7], 4, spare=3)
+    t.rows_for(0)
+    for batch, offsets in ((0, [0, CANARY, CANARY]), (1, [0, 0, CANARY])):
+        t.h.cache_extend(t.change.data_ptr(), t.d_lens.data_ptr(), t.d_table.data_ptr(), batch, t.d_stack.data_ptr(), t.d_count.data_ptr(),
+                         t.q_off.data_ptr(), 0, 0, 0, t.err.data_ptr(), t.torch.cuda.current_stream().cuda_stream)
+        assert int(t.err) == 0 and t.q_off.cpu().tolist() == offsets
+        t.h.cache_trim(t.d_lens.clone().data_ptr(), t.d_lens.data_ptr(), t.d_table.data_ptr(), batch, t.d_stack.data_ptr(), t.d_count.data_ptr(),
+                       t.err.data_ptr(), t.torch.cuda.current_stream().cuda_stream)
+        t.check_state()
+    assert int(t.err) == 0
+    t.h.close()
+
+
 @pytest.mark.parametrize("what", ["pages", "row of the table", "rows", "negative", "negative length", "count", "huge"])
 def test_extend_refused_on_the_device(lib, what):
     """Nothing changes but the error word, and the batch has no new rows."""
