@@ -673,18 +673,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
       };
-      auto write_rows = [&](auto address) {   // address(token, head, row): where the row's kRowBytes go
+      // first[row of the warp]: where in `to` the row's kRowBytes go, held by the row's lane
+      auto write_rows = [&](uint8_t* to, int64_t first) {
         __syncwarp();
-#pragma unroll 2
+#pragma unroll 4
         for (int i = 0; i < kRowLanes; ++i) {
           const int r = i * (32 / kRowLanes) + lane / kRowLanes, vec = lane % kRowLanes;
-          const int r_item = warp_row + r;
-          if (r_item < x.n_rows) {
-            int token_r, head_r;
-            rows_out.at(p, r_item, token_r, head_r);
-            reinterpret_cast<uint4*>(address(token_r, head_r, r_item))[vec] =
-                ld_shared(out_stage + uint32_t(r) * kRowBytes + uint32_t((vec ^ (r & 7)) << 4));
-          }
+          const int64_t at = __shfl_sync(0xffffffffu, first, r);
+          const uint4 v = ld_shared(out_stage + uint32_t(r) * kRowBytes + uint32_t((vec ^ (r & 7)) << 4));
+          if (warp_row + r < x.n_rows) reinterpret_cast<uint4*>(to + at)[vec] = v;
         }
         __syncwarp();
       };
@@ -700,9 +697,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                                  pack<true>(o[8 * i + 4], o[8 * i + 5]), pack<true>(o[8 * i + 6], o[8 * i + 7])));
           }
         }
-        write_rows([&](int token_r, int head_r, int) {
-          return p.out + ((int64_t(x.q_start) + token_r) * p.num_q_heads + x.head * p.group + head_r) * D;
-        });
+        write_rows(reinterpret_cast<uint8_t*>(p.out), out_row * kRowBytes);
       } else {
 #pragma unroll 1
         for (int half = 0; half < kHalves; ++half) {
@@ -717,9 +712,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                                    __float_as_uint(o[4 * i + 3])));
             }
           }
-          write_rows([&](int, int, int r_item) {
-            return p.partial_o + ((int64_t(x.slot) + r_item) * p.num_kv_heads + x.head) * D + half * (D / 2);
-          });
+          write_rows(reinterpret_cast<uint8_t*>(p.partial_o), (part_row * 2 + half) * kRowBytes);
         }
       }
     } while (false);
