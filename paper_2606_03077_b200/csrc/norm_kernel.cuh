@@ -365,7 +365,6 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
   const int R = p.rope.rotary_dim, pairs = R / 2;
   for (int i = threadIdx.x; i < pairs; i += kNormThreads) turns[i] = p.rope.turns[i];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  __syncthreads();
   const int lanes = 1 << p.lanes_shift, item = lane & (lanes - 1), group = lane >> p.lanes_shift, groups_shift = 5 - p.lanes_shift, groups = 1 << groups_shift;
   const bool on = item < p.items;
   const Item<V, kHalf> it(item, p.items, R);
@@ -375,7 +374,6 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
   if (kAppend && p.n_rows) n_tokens = max(int64_t(0), min(n_tokens, int64_t(*p.n_rows)));
   const Run run(n_tokens, p.steps, gridDim.x * kNormWarps, blockIdx.x * kNormWarps + warp);
   int left = run.left;
-  if (left == 0) return;
 
   struct Part {   // of the run: heads of one token and one kind
     int kind, head0, steps, rows;   // this lane's first head, steps, rows of this lane's group
@@ -437,7 +435,8 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_rope_kernel(co
     copies_commit();
   }
 
-  int32_t pos = pairs > 0 ? p.positions[token] : 0, slot = kAppend ? p.slots[token] : 0;
+  int32_t pos = pairs > 0 && left > 0 ? p.positions[token] : 0, slot = kAppend && left > 0 ? p.slots[token] : 0;
+  __syncthreads();   // `turns`, while the first rows are on their way
   bool new_token = true;
   uint32_t place = 0;
 #pragma unroll 1
@@ -568,7 +567,6 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
   const int R = p.rope.rotary_dim, pairs = R / 2;
   for (int i = threadIdx.x; i < pairs; i += kThreads) turns[i] = p.rope.turns[i];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  __syncthreads();
   const int lanes = 1 << p.lanes_shift, item = lane & (lanes - 1), group = lane >> p.lanes_shift, groups_shift = 5 - p.lanes_shift, groups = 1 << groups_shift;
   const bool on = item < p.items;
   const Item<V, kHalf> it(item, p.items, R);
@@ -637,6 +635,7 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
     copies_commit();
   }
   int32_t pos = pairs > 0 && left > 0 ? p.positions[token] : 0;
+  __syncthreads();   // `turns`, while the first rows are on their way
   bool new_token = true;
   uint32_t place = 0;
 #pragma unroll 1
