@@ -23,7 +23,7 @@
 // Measured (device, changing inputs): 8191 tokens of 40 + 8 heads of 128, fp16, half of each rotated, 36 us = 5.6 TB/s; gradient of 16384
 // tokens of 32 + 8 heads, bf16, 83 us = 6.1 TB/s, of which 2 - 3 are the sums of the blocks (a kernel of its own); 16K tokens of 64 + 8 heads
 // into an E4M3 cache 109 us = 5.8 TB/s.  A step is 215 instructions forward and 310 backward; with few heads a token's own share of
-// them (factors, addresses) shows: 8192 tokens of 16 + 4 heads 20 us, 4.2 TB/s.  q and k of 64 tokens: 2.9 us.
+// them (factors, addresses) shows: 8192 tokens of 16 + 4 heads 20 us, 4.2 TB/s.  q and k of 64 tokens: 2.8 us.
 // What did not do as well, on the three above (us): rows straight into registers, two a lane 41 / 128 / 157 (spills), four 43 / 158 / 143;
 // every 32nd row a warp's, with the factors in shared memory 55 / 134 / 208; interleaved items of two neighbouring vectors 53 for the
 // first (each sector asked for twice); gradient blocks for q or k alone 106.
