@@ -15,7 +15,7 @@
 // count change in place: the first block writes them once all have read them (cluster barrier).
 //
 // What bounds it: latency; in long batches the instructions of eight multiprocessors.  A step of 64 sequences, extend and trim: 6 us
-// together; 256 sequences with 115K new tokens: 13 us together (a row a thread 18, four rows 14.5).
+// together; 256 sequences with 115K new tokens: 13 us together.
 #pragma once
 #include <cuda_runtime.h>
 
@@ -183,8 +183,8 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const Ta
   if (threadIdx.x == 0) row_begin[p.batch] = rows;
   __syncthreads();
   if (ranks > 1) cluster_arrive();   // this block has read the lengths and the count
-  // A row a thread while there are threads enough (64 rows: 2.9 us against 3.3 with four a thread), else kTableRows (115K rows: 9 us against
-  // 14 with one), with whole vectors written where the arrays lie on them.
+  // A row a thread while there are threads enough (64 sequences, extend and trim: 6.0 us, with kTableRows 9.0), else kTableRows (115K rows: 13.0
+  // us, with one 32), with whole vectors written where the arrays lie on them.
   const int64_t threads = int64_t(ranks) * blockDim.x;
   const int per = rows > threads ? kTableRows : 1;
   const bool vectors = per > 1 && ((reinterpret_cast<uintptr_t>(p.positions) | reinterpret_cast<uintptr_t>(p.slots)) & 15) == 0;
