@@ -606,14 +606,16 @@ int libra_chunk_attn(libra_handle_t handle, const void* q, int64_t q_stride, con
  *                            more pages going back than the pool has room for
  *   LIBRA_ERR_PLAN_OVERFLOW  a length past the end of a block-table row (or past 2^31 - 1), more than max_rows new rows
  *   LIBRA_ERR_NO_PAGES       more pages needed than there are
- * Page ids are handed on as they are; the calls that use them check them.
+ * Page ids are handed on as they are; the calls that use them check them.  Slots of a page whose id is outside the pool are
+ * below -1, whatever the id: libra_norm_rope_append reports those rows and does not store them.
  *
  * libra_cache_extend: sequence b, of seq_lens[b] tokens, gets new_tokens[b] more (0 allowed).  The pages it needs for them are taken
  * from the top of the stack - the k-th of the batch, in the order of the sequences and of their pages, is
  * free_pages[*free_count - 1 - k] - and written into its row of the block table.  Then, with the lengths before the call,
  *   q_offsets[b]   int32[batch + 1]: sum of new_tokens over the sequences before b (the packed rows of the calls below)
  *   positions[r]   int32[max_rows] or NULL: seq_lens[b] + i for row r = q_offsets[b] + i
- *   slots[r]       int32[max_rows] or NULL: page * page_size + position % page_size, page = block_table[b][position / page_size]
+ *   slots[r]       int32[max_rows] or NULL: page * page_size + position % page_size, page = block_table[b][position / page_size]; a
+ *                  number below -1 where that is not in [0, num_pages)
  * and seq_lens[b] grows by new_tokens[b].  Rows behind q_offsets[batch] are left as they were.
  *
  * libra_cache_trim: sequence b keeps its first keep_lens[b] tokens (0: it has ended); seq_lens[b] becomes that, and the pages from

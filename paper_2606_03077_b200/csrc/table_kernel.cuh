@@ -2,7 +2,7 @@
 //
 //   extend  sequence b of L_b tokens gets n_b more:  w_b = ceil((L_b + n_b) / P) - ceil(L_b / P) pages, in the order of the batch
 //           and of the pages; the k-th of them all is free[count - 1 - k].  Row q_offsets[b] + i is token t = L_b + i, in slot
-//           page(t / P) * P + t % P.
+//           page(t / P) * P + t % P; a page whose id is outside the pool has numbers below -1 for slots, which whoever uses them reports.
 //   trim    sequence b keeps its first m_b tokens: pages from ceil(m_b / P) on go back; the k-th of the F of them is
 //           free[count + F - 1 - k], so that what extend has taken trim puts back in the order it was.
 //
@@ -110,6 +110,12 @@ __device__ __forceinline__ int32_t pages_of(int32_t len, int page_shift) {
   return int32_t((uint32_t(len) + (1u << page_shift) - 1) >> page_shift);
 }
 
+// A page's first slot.  That of an id outside the pool: such that all of the page's are negative and none is -1, which asks for a row
+// not to be stored.  (The id times the page size may be a good slot in 32 bits, and for id -1 the page's last slot is -1.)
+__device__ __forceinline__ int32_t first_slot(int32_t id, const TableParams& p) {
+  return uint32_t(id) < uint32_t(p.num_pages) ? id << p.page_shift : -(1 << p.page_shift) - 1;   // there are fewer than 2^27 pages
+}
+
 // The last i in [0, n) with begins[i] <= x; begins[0] <= x.
 __device__ __forceinline__ int owner_of(const int32_t* begins, int n, int32_t x) {
   int lo = 0, hi = n;
@@ -204,11 +210,12 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const Ta
       const int32_t id1 = page1 == page0 ? id0 : (page1 >= had ? stack[-page1] : row[page1]);
       if (page0 >= had && (first & (P - 1)) == 0) row[page0] = id0;
       if (page1 != page0 && page1 >= had) row[page1] = id1;
+      const int32_t slots0 = first_slot(id0, p), slots1 = first_slot(id1, p);
 #pragma unroll
       for (int k = 0; k < kTableRows; ++k) {
         if (k >= i && k < i + m) {
           pos[k] = first + (k - i);
-          slot[k] = int32_t(uint32_t(pos[k] >> p.page_shift == page0 ? id0 : id1) << p.page_shift) + (pos[k] & (P - 1));
+          slot[k] = (pos[k] >> p.page_shift == page0 ? slots0 : slots1) + (pos[k] & (P - 1));
         }
       }
       i += m;
