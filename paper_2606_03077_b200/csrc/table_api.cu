@@ -46,7 +46,9 @@ int launch_table(libra_handle_t h, void (*fn)(libra::TableParams), const libra::
   DeviceGuard guard(h->cfg.device);
   if (guard.err != cudaSuccess) return fail_cuda(h, guard.err);
   if (smem > 40 * 1024) {   // beside the static part
-    LIBRA_CUDA_TRY(h, cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    // not this call's bytes but the most: the limit is the process's, and a call on another thread must not find it below its own
+    constexpr size_t most = (3 * size_t(libra::kTableMaxBatch) + 1) * sizeof(int32_t);
+    LIBRA_CUDA_TRY(h, cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)));
   }
   int64_t threads = std::max(1, (p.batch + libra::kTablePerThread - 1) / libra::kTablePerThread);
   threads = std::max<int64_t>(threads, std::min<int64_t>(work, libra::kTableMaxThreads));
