@@ -18,6 +18,7 @@ using libra::NormKind;
 using libra::NormParams;
 
 constexpr int kMaxHeads = 16384;
+constexpr int kMaxDim = 1024;
 constexpr int kMostBlocks = 8;       // a multiprocessor, of the gradient's sums: sizes its workspace
 
 bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
@@ -100,7 +101,7 @@ int check_call(int32_t device, const libra_rope_t* rope, int32_t dtype, const in
   if (device < 0 || n_tokens < 0 || head_dim <= 0 || dtype < LIBRA_ROPE_BF16 || dtype > LIBRA_ROPE_F32) return LIBRA_INVALID_ARGUMENT;
   if (rope && (!valid_rope(rope) || !positions)) return LIBRA_INVALID_ARGUMENT;
   if (!aligned(positions, 4) || !std::isnormal(eps) || eps < 0.f) return LIBRA_INVALID_ARGUMENT;
-  if (head_dim % 2 != 0 || head_dim > 1024 || (rope && rope->rotary_dim > head_dim) || n_tokens > 0x7fffffff) return LIBRA_UNSUPPORTED_SHAPE;
+  if (head_dim % 2 != 0 || head_dim > kMaxDim || (rope && rope->rotary_dim > head_dim) || n_tokens > 0x7fffffff) return LIBRA_UNSUPPORTED_SHAPE;
   return LIBRA_OK;
 }
 
@@ -173,7 +174,7 @@ int libra_norm_rope_apply(int32_t device, const libra_rope_t* rope, const libra_
 
 int libra_norm_rope_workspace_size(int32_t device, int32_t head_dim, size_t* bytes) {
   if (device < 0 || head_dim <= 0 || !bytes) return LIBRA_INVALID_ARGUMENT;
-  if (head_dim % 2 != 0 || head_dim > 1024) return LIBRA_UNSUPPORTED_SHAPE;
+  if (head_dim % 2 != 0 || head_dim > kMaxDim) return LIBRA_UNSUPPORTED_SHAPE;
   int n_sm = 0;
   if (sm_count(device, &n_sm) != LIBRA_OK) return LIBRA_CUDA_ERROR;
   *bytes = size_t(n_sm) * kMostBlocks * 2 * head_dim * sizeof(float);
@@ -244,10 +245,14 @@ int libra_norm_rope_gradient(int32_t device, const libra_rope_t* rope, const lib
                                               : gradient_fn<float, 4>(vec, wide, half);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int kinds = k ? 2 : 1;
-  const size_t row = size_t(head_dim) * sizeof(float);
-  const size_t smem = size_t(warps) * (by_lanes ? std::max<size_t>(libra::kNormGradAhead * libra::kNormGradStepBytes, kinds * row) : (2 + kinds) * row);
+  // a warp's: the ring, which also holds the sums of both kinds at the end, or rows of float32 (x, the gradient, each kind's sums)
+  constexpr size_t ring = libra::kNormGradAhead * libra::kNormGradStepBytes, row = kMaxDim * sizeof(float);
+  static_assert(2 * 32 * 16 * sizeof(float) <= ring, "the sums of two kinds: rows of 32 items of two vectors of eight channels at most");
+  const size_t smem = size_t(warps) * (by_lanes ? ring : (2 + kinds) * size_t(head_dim) * sizeof(float));
   if (smem > 40 * 1024) {   // beside the static part
-    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    // not this call's bytes but the most of the kernel: the limit is the process's, and a call on another thread must not find it below its own
+    const size_t most = size_t(warps) * (by_lanes ? ring : 4 * row);
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
     if (e != cudaSuccess) return fail_cuda(nullptr, e);
   }
   cudaError_t e = libra::launch(true, 1, fn, dim3(blocks), unsigned(warps * 32), smem, st, p);

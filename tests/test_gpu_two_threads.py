@@ -42,3 +42,17 @@ def test_extend_of_two_long_batches(lib):
     for k in keep:
         assert int(k[7]) == 0
         k[0].close()
+
+
+def test_gradients_through_shared_memory(lib):
+    import torch
+    keep, calls = [], []
+    for dim in (1022, 702):   # rows that no 16-byte vector divides; q and k
+        x, g, o = (torch.ones((3, 1, dim), device="cuda") for _ in range(3))
+        k_out, w, gw, gw_k = torch.ones((3, 1, dim), device="cuda"), *(torch.ones(dim, device="cuda") for _ in range(3))
+        ws, st = torch.empty(lib.libra_norm_rope_workspace_size(0, dim), dtype=torch.uint8, device="cuda"), torch.cuda.Stream()
+        q, k = lib.NormGrads.of(x, g, w, o, gw), lib.NormGrads.of(x, g, w, k_out, gw_k)
+        keep.append((x, g, o, k_out, w, gw, gw_k, ws, st))
+        calls.append(lambda q=q, k=k, dim=dim, ws=ws, st=st: lib.libra_norm_rope_gradient(
+            0, None, q, k, lib.ROPE_F32, 0, 3, dim, 1e-6, ws.data_ptr(), ws.numel(), st.cuda_stream))
+    together(*calls)
