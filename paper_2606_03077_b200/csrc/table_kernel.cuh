@@ -263,10 +263,9 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_trim_kernel(const Tabl
     const bool live = b0 + i < p.batch;
     len[i] = live ? p.seq_lens[b0 + i] : 0;
     keep[i] = live ? p.change[b0 + i] : 0;
-    if (keep[i] < 0 || keep[i] > len[i] || len[i] > most) {
-      bad |= LIBRA_ERR_BAD_LENGTH;
-      len[i] = keep[i] = 0;
-    }
+    if (len[i] > most) bad |= LIBRA_ERR_PLAN_OVERFLOW;
+    if (keep[i] < 0 || keep[i] > len[i]) bad |= LIBRA_ERR_BAD_LENGTH;
+    if (bad) len[i] = keep[i] = 0;
     stay[i] = pages_of(keep[i], p.page_shift);
     gone[i] = pages_of(len[i], p.page_shift) - stay[i];
     mine.rows += gone[i];
