@@ -141,7 +141,8 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const Ta
   const int b0 = threadIdx.x * kTablePerThread, P = 1 << p.page_shift;
   const int64_t most = min(int64_t(p.block_table_ld) << p.page_shift, int64_t(0x7fffffff));   // that a row describes
   const int32_t count = *p.free_count;
-  uint32_t bad = count < 0 || count > p.num_pages ? LIBRA_ERR_BAD_LENGTH : 0u;
+  const bool counted = count >= 0 && count <= p.num_pages;
+  uint32_t bad = counted ? 0u : LIBRA_ERR_BAD_LENGTH;
   int32_t len[kTablePerThread], add[kTablePerThread], want[kTablePerThread];
   Sums mine = {0, 0};
 #pragma unroll
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const Ta
   Sums total;
   Sums at = block_scan(mine, (p.batch + 32 * kTablePerThread - 1) / (32 * kTablePerThread), total);
   if (total.rows > p.max_rows) bad |= LIBRA_ERR_PLAN_OVERFLOW;
-  else if (total.pages > count) bad |= LIBRA_ERR_NO_PAGES;
+  else if (counted && total.pages > count) bad |= LIBRA_ERR_NO_PAGES;
   // every block comes to the same verdict
   const bool refused = __syncthreads_or(int(bad)) != 0;
   if (refused) {   // nothing changes, and the batch has no new rows

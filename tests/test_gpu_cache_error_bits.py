@@ -24,3 +24,19 @@ def test_trim_past_the_end_of_a_row(lib, length, keep, bits):
     assert int(t.err) == sum(getattr(lib, "ERR_" + b) for b in bits.split())
     unchanged(t)
     t.h.close()
+
+
+@pytest.mark.parametrize("new,count,bits", [([0, 0, 0], -1, "BAD_LENGTH"), ([1, 1, 1], -1, "BAD_LENGTH"), ([30, 30, 0], -2 ** 31, "BAD_LENGTH"),
+                                            ([12, 33, 0], 1000, "BAD_LENGTH"), ([12, 33, 1], None, "NO_PAGES"), ([0, 0, 57], None, "PLAN_OVERFLOW"),
+                                            ([11, 20, 30], None, "PLAN_OVERFLOW"), ([1, -1, 1], None, "BAD_LENGTH"),
+                                            ([2 ** 31 - 1] * 3, None, "PLAN_OVERFLOW"), ([-1, 0, 57], None, "BAD_LENGTH PLAN_OVERFLOW")])
+def test_extend(lib, new, count, bits):
+    t = Tables(lib, [5, 16, 40], 6, spare=3)
+    t.rows_for(60)
+    if count is not None:
+        t.d_count[0] = t.count = count
+    t.extend(new)
+    assert int(t.err) == sum(getattr(lib, "ERR_" + b) for b in bits.split())
+    unchanged(t)
+    assert t.q_off[:4].tolist() == [0, 0, 0, 0]
+    t.h.close()
