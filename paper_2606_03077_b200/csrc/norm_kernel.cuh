@@ -285,11 +285,12 @@ __device__ __forceinline__ float group_sum(float x, int lanes) {
   return y[0];
 }
 
-// 1 / sqrt(m): the approximation and a Newton step; 0 for infinity
+// 1 / sqrt(m): the approximation and a Newton step; 0 for infinity.  m r first, which is a normal number: half of the smallest m is none
+// and would be flushed to zero.
 __device__ __forceinline__ float inverse_root(float m) {
   float r;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(m));
-  const float better = r * fmaf(-0.5f * m * r, r, 1.5f);
+  const float better = r * fmaf(-0.5f * (m * r), r, 1.5f);
   return m == INFINITY ? 0.f : better;
 }
 
