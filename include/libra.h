@@ -635,8 +635,8 @@ int libra_cache_trim(libra_handle_t handle, const int32_t* keep_lens, int32_t* s
  *     r = 1 / sqrt(mean(x^2) + eps),   y = rotation(w * x * r)      (rotary positions as above; rope NULL: none)
  * and, for the gradient dy of y,   g = transposed rotation(dy),   dx = r * (w * g - x * r * mean(w * g * x * r)),
  *     dw = sum over tokens and heads of g * x * r.
- * Arithmetic in float32, one rounding to the type; dw is float32.  x^2 is summed in float32: its mean must be finite there, and
- * where it is below the smallest normal number it counts as zero.  eps is a positive, normal float32.
+ * Arithmetic in float32, one rounding to the type; dw is float32.  x^2 is summed in float32: a head whose sum is not finite there
+ * has r = 0 (zeros; NaN where x is infinite or NaN), and a mean below the smallest normal number counts as zero.  eps is a positive, normal float32.
  *
  * libra_norm_rows_t describes q or k as device arrays [n_tokens, n_heads, head_dim] of `dtype` (LIBRA_ROPE_BF16 ...), element (t, h,
  * c) at t * stride_token + h * stride_head + c; weight: [head_dim] of `dtype`.  out may be x (with the same strides); any other

@@ -1,5 +1,5 @@
-"""Norms at the ends of what float32 holds: epsilons next to the smallest normal number.  Bounds as derived in test_gpu_norm_rope.py; rows
-held by a group of lanes (64 channels) and through shared memory (30 channels)."""
+"""Norms at the ends of what float32 holds: epsilons next to the smallest normal number, squares whose sum has no place in
+float32.  Bounds as derived in test_gpu_norm_rope.py; rows held by a group of lanes (64 channels) and through shared memory (30 channels)."""
 import numpy as np
 import pytest
 
@@ -42,3 +42,24 @@ def test_the_smallest_epsilons(lib, eps, dim, dtype):
     # zeros; rows whose squares count as zero beside epsilon; rows that decide alone
     x *= np.array([0.0, 2.0 ** -80, 1.0, 0.0, 2.0 ** -40, 2.0 ** 40])[:, None, None]
     run(lib, x, g, w, dtype, eps)
+
+
+@pytest.mark.parametrize("dim", [64, 30])
+def test_rows_whose_squares_have_no_sum(lib, dim):
+    """Zeros for the row, which adds nothing to the weight's gradient, NaN for a channel that is infinite, and its own row alone."""
+    import torch
+    x, g = (torch.ones((3, 4, dim), device="cuda") for _ in range(2))
+    x[0, 2], x[2, 0], x[2, 1] = 2.0 ** 70, 2.0 ** 62.5, -2.0 ** 63      # the means of the last two have a place in float32
+    w, out, gx, gw = torch.ones(dim, device="cuda"), torch.empty_like(x), torch.empty_like(x), torch.empty(dim, device="cuda")
+    ws = torch.empty(lib.libra_norm_rope_workspace_size(0, dim), dtype=torch.uint8, device="cuda")
+    lib.libra_norm_rope_apply(0, None, lib.NormRows.of(x, w, out), None, lib.ROPE_F32, 0, 3, dim, 1e-6, stream())
+    lib.libra_norm_rope_gradient(0, None, lib.NormGrads.of(x, g, w, gx, gw), None, lib.ROPE_F32, 0, 3, dim, 1e-6, ws.data_ptr(), ws.numel(), stream())
+    past = x.abs()[..., 0] > 1
+    assert bool((out[past] == 0).all()) and bool((gx[past] == 0).all())
+    # 1 / sqrt(1 + 1e-6) = 1 - 5e-7 for the others, each of them g x r; steps of 2^-24 (dim / 2 of them at most, and nine additions)
+    assert bool(((out[~past] - 1).abs() <= 1e-6 + dim * U).all()) and bool(((gw - 9).abs() <= 9 * (1e-6 + dim * U)).all())
+    x[1, 3, 5], x[0, 0, 7] = float("inf"), float("nan")
+    lib.libra_norm_rope_apply(0, None, lib.NormRows.of(x, w, out), None, lib.ROPE_F32, 0, 3, dim, 1e-6, stream())
+    bad = torch.isnan(out)
+    assert bad[1, 3].tolist() == [c == 5 for c in range(dim)] and bool((out[1, 3][~bad[1, 3]] == 0).all())
+    assert bool(bad[0, 0].all()) and int(bad.sum()) == dim + 1
