@@ -5,7 +5,7 @@
 //   g = R(a)^T dy,   dw = sum over tokens and heads of g x r,   dx = r (w g - x r mean(w g x r))
 //
 // Arithmetic in float32, one rounding to the type.  Neither r nor the normalised x is kept for the gradient: x has to be read there
-// in any case.  The two sums of a row of the gradient, of x^2 and of w g x, are found in the same pass.
+// in any case.  A row of the gradient takes two sums, of x^2 and then of w g x r: every value on the way is one of the formula's.
 //
 // Every byte moves once; memory bounds it.  A step is the rows (heads) of one token and one kind (q, k, v) that a warp holds at once: a
 // row is held by a group of neighbouring lanes, each with one item of two vectors (of 16 bytes, or 8) whose channels turn together (half layout:
@@ -692,25 +692,22 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
         gb[k] = fma2(gb[k], c, mul2(ga[k], minus(s)));
         ga[k] = g;
       }, [](int) {});
-      // sums of x^2 and, from the products g x, of w g x
-      float2 square = both(0.f), dot = both(0.f), more = both(0.f), dots = both(0.f);
+      float2 square = both(0.f), more = both(0.f);
 #pragma unroll
       for (int k = 0; k < V / 2; ++k) {
         square = fma2(xa[k], xa[k], square);
         more = fma2(xb[k], xb[k], more);
-        dot = fma2(mul2(ga[k], xa[k]), wa[k], dot);
-        dots = fma2(mul2(gb[k], xb[k]), wb[k], dots);
       }
-      float sum[2] = {(square.x + more.x) + (square.y + more.y), (dot.x + dots.x) + (dot.y + dots.y)};
-      group_sums(sum, lanes);
-      const float r = inverse_root(fmaf(sum[0], p.inv_dim, p.eps));
-      const float2 r2 = both(r), mean2 = both(-(sum[1] * p.inv_dim * r));   // minus the mean of w g x r
-      if (j < x.rows) {
+      const float r = inverse_root(fmaf(group_sum((square.x + more.x) + (square.y + more.y), lanes), p.inv_dim, p.eps));
+      const float2 r2 = both(r);
+      const bool there = j < x.rows;
+      // x r and w g take the places of x and g; the sum of w g x r is of these: w g x may have no place in float32 where they do
 #pragma unroll
-        for (int k = 0; k < V / 2; ++k) {
-          xa[k] = mul2(xa[k], r2);
-          xb[k] = mul2(xb[k], r2);
-        }
+      for (int k = 0; k < V / 2; ++k) {
+        xa[k] = mul2(xa[k], r2);
+        xb[k] = mul2(xb[k], r2);
+      }
+      if (there) {
         if (x.kind == 0) {
 #pragma unroll
           for (int k = 0; k < V / 2; ++k) {
@@ -724,10 +721,21 @@ __global__ void __launch_bounds__(kNormGradThreads<T>, 1) norm_rope_gradient_ker
             accb[1][k] = fma2(gb[k], xb[k], accb[1][k]);
           }
         }
+      }
+      float2 dot = both(0.f), dots = both(0.f);
+#pragma unroll
+      for (int k = 0; k < V / 2; ++k) {
+        ga[k] = mul2(ga[k], wa[k]);
+        gb[k] = mul2(gb[k], wb[k]);
+        dot = fma2(ga[k], xa[k], dot);
+        dots = fma2(gb[k], xb[k], dots);
+      }
+      const float2 mean2 = both(-(group_sum((dot.x + dots.x) + (dot.y + dots.y), lanes) * p.inv_dim));   // minus the mean of w g x r
+      if (there) {
 #pragma unroll
         for (int k = 0; k < V / 2; ++k) {
-          ga[k] = mul2(fma2(xa[k], mean2, mul2(ga[k], wa[k])), r2);
-          gb[k] = mul2(fma2(xb[k], mean2, mul2(gb[k], wb[k])), r2);
+          ga[k] = mul2(fma2(xa[k], mean2, ga[k]), r2);
+          gb[k] = mul2(fma2(xb[k], mean2, gb[k]), r2);
         }
         from_pairs<V, kHalf>(ga, gb, v0, v1);
         Raw<T, V>(v0).store(out + it.c0);
@@ -942,13 +950,13 @@ __global__ void __launch_bounds__(kNormAnyThreads) norm_rope_gradient_any_kernel
       const float2 z = second ? rope::turned(gs[other], gs[ch], b) : rope::turned(gs[ch], gs[other], b);
       return second ? z.y : z.x;
     };
-    float dot = 0.f;
+    const float r = __frsqrt_rn(fmaf(group_sum(square, 32), p.inv_dim, p.eps));
+    float dot = 0.f;   // of w g x r; w g x may have no place in float32
     for (int c = lane * V; c < D; c += 32 * V) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) dot = fmaf(mul_rn(back(c + i), rope::to_f32(weight[c + i])), xs[c + i], dot);
+      for (int i = 0; i < V; ++i) dot = fmaf(mul_rn(back(c + i), rope::to_f32(weight[c + i])), mul_rn(xs[c + i], r), dot);
     }
-    const float r = __frsqrt_rn(fmaf(group_sum(square, 32), p.inv_dim, p.eps));
-    const float mean = mul_rn(mul_rn(group_sum(dot, 32), p.inv_dim), r);
+    const float mean = mul_rn(group_sum(dot, 32), p.inv_dim);
     for (int c = lane * V; c < D; c += 32 * V) {
       alignas(16) T t[V];
 #pragma unroll

@@ -1,5 +1,6 @@
 """Norms at the ends of what float32 holds: epsilons next to the smallest normal number, squares whose sum has no place in
-float32.  Bounds as derived in test_gpu_norm_rope.py; rows held by a group of lanes (64 channels) and through shared memory (30 channels)."""
+float32, gradients whose product with x has none although every term of the result has one.  Bounds as derived in
+test_gpu_norm_rope.py; rows held by a group of lanes (64 channels) and through shared memory (30 channels)."""
 import numpy as np
 import pytest
 
@@ -63,3 +64,14 @@ def test_rows_whose_squares_have_no_sum(lib, dim):
     bad = torch.isnan(out)
     assert bad[1, 3].tolist() == [c == 5 for c in range(dim)] and bool((out[1, 3][~bad[1, 3]] == 0).all())
     assert bool(bad[0, 0].all()) and int(bad.sum()) == dim + 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [64, 30])
+@pytest.mark.parametrize("x_scale,g_scale,w_scale", [(-50, -80, 0), (-50, -99, 0), (58, 75, 0), (60, 90, -5), (20, 110, 3), (-40, -60, -25), (0, 0, 0)])
+def test_gradients_far_from_one(lib, x_scale, g_scale, w_scale, dim, dtype):
+    rng = np.random.default_rng(100 + dim - x_scale)
+    x, g, w = (rng.standard_normal(s) * 2.0 ** k for s, k in (((5, 3, dim), x_scale), ((5, 3, dim), g_scale), (dim, w_scale)))
+    if g_scale + w_scale < 70:   # dx of a row of zeros is 2^50 w g: 2^125 and more at the others' scales, of which elements pass 2^128
+        x[1, 1] = 0.0
+    run(lib, x, g, w, dtype, 2.0 ** -100)
