@@ -641,9 +641,10 @@ int libra_cache_trim(libra_handle_t handle, const int32_t* keep_lens, int32_t* s
  * libra_norm_rows_t describes q or k as device arrays [n_tokens, n_heads, head_dim] of `dtype` (LIBRA_ROPE_BF16 ...), element (t, h,
  * c) at t * stride_token + h * stride_head + c; weight: [head_dim] of `dtype`.  out may be x (with the same strides); any other
  * overlap is not allowed, and the rows of out do not overlap (tokens apart by all heads of one, or heads by all tokens of one).
- * k NULL: q alone.  positions: int32[n_tokens] on the device (NULL allowed without rope).  head_dim is even, rotary_dim <= head_dim <=
- * 1024, n_heads <= 16384; rows need no more than the element's own alignment (16-byte aligned ones are faster).  Asynchronous on
- * `stream`; nothing is allocated; may be recorded.  Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE, CUDA_ERROR. */
+ * k NULL: q alone.  positions: int32[n_tokens] on the device (NULL allowed without rope).  For no tokens rows and positions may be
+ * NULL, as the addresses of empty arrays are.  head_dim is even, rotary_dim <= head_dim <= 1024, n_heads <= 16384; rows need no more than
+ * the element's own alignment (16-byte aligned ones are faster).  Asynchronous on `stream`; nothing is allocated; may be recorded.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_SHAPE, CUDA_ERROR. */
 typedef struct {
   const void* x;
   void* out;

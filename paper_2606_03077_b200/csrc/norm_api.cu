@@ -99,7 +99,7 @@ NormFn append_fn(int v, bool half) {   // the handle's strides and addresses are
 int check_call(int32_t device, const libra_rope_t* rope, int32_t dtype, const int32_t* positions, int64_t n_tokens, int32_t head_dim,
                float eps) {
   if (device < 0 || n_tokens < 0 || head_dim <= 0 || dtype < LIBRA_ROPE_BF16 || dtype > LIBRA_ROPE_F32) return LIBRA_INVALID_ARGUMENT;
-  if (rope && (!valid_rope(rope) || !positions)) return LIBRA_INVALID_ARGUMENT;
+  if (rope && (!valid_rope(rope) || (!positions && n_tokens > 0))) return LIBRA_INVALID_ARGUMENT;
   if (!aligned(positions, 4) || !std::isnormal(eps) || eps < 0.f) return LIBRA_INVALID_ARGUMENT;
   if (head_dim % 2 != 0 || head_dim > kMaxDim || (rope && rope->rotary_dim > head_dim) || n_tokens > 0x7fffffff) return LIBRA_UNSUPPORTED_SHAPE;
   return LIBRA_OK;
@@ -134,11 +134,11 @@ int libra_norm_rope_apply(int32_t device, const libra_rope_t* rope, const libra_
   for (int i = 0; i < 2; ++i) {
     const libra_norm_rows_t* t = i ? k : q;
     if (!t) continue;
-    if (!t->x || !t->out || !t->weight || t->n_heads <= 0) return LIBRA_INVALID_ARGUMENT;
+    if (!t->weight || t->n_heads <= 0 || (n_tokens > 0 && (!t->x || !t->out))) return LIBRA_INVALID_ARGUMENT;
     if (t->x_stride_token < 0 || t->x_stride_head < 0 || t->out_stride_token < 0 || t->out_stride_head < 0) return LIBRA_INVALID_ARGUMENT;
     if (!aligned(t->x, eb) || !aligned(t->out, eb) || !aligned(t->weight, eb)) return LIBRA_INVALID_ARGUMENT;
     if (!rows_apart(n_tokens, t->n_heads, head_dim, t->out_stride_token, t->out_stride_head)) return LIBRA_INVALID_ARGUMENT;
-    if (t->x == t->out && (t->x_stride_token != t->out_stride_token || t->x_stride_head != t->out_stride_head)) return LIBRA_INVALID_ARGUMENT;
+    if (t->x && t->x == t->out && (t->x_stride_token != t->out_stride_token || t->x_stride_head != t->out_stride_head)) return LIBRA_INVALID_ARGUMENT;
     if (t->n_heads > kMaxHeads) return LIBRA_UNSUPPORTED_SHAPE;
     NormKind& kind = p.kind[i];
     kind.x = t->x;
@@ -194,7 +194,8 @@ int libra_norm_rope_gradient(int32_t device, const libra_rope_t* rope, const lib
   for (int i = 0; i < 2; ++i) {
     const libra_norm_grads_t* t = i ? k : q;
     if (!t) continue;
-    if (!t->x || !t->grad_out || !t->weight || !t->grad_x || !t->grad_weight || t->n_heads <= 0) return LIBRA_INVALID_ARGUMENT;
+    if (!t->weight || !t->grad_weight || t->n_heads <= 0) return LIBRA_INVALID_ARGUMENT;
+    if (n_tokens > 0 && (!t->x || !t->grad_out || !t->grad_x)) return LIBRA_INVALID_ARGUMENT;   // no row is read without tokens
     if (t->x_stride_token < 0 || t->x_stride_head < 0 || t->grad_out_stride_token < 0 || t->grad_out_stride_head < 0 ||
         t->grad_x_stride_token < 0 || t->grad_x_stride_head < 0) {
       return LIBRA_INVALID_ARGUMENT;
@@ -203,8 +204,8 @@ int libra_norm_rope_gradient(int32_t device, const libra_rope_t* rope, const lib
       return LIBRA_INVALID_ARGUMENT;
     }
     if (!rows_apart(n_tokens, t->n_heads, head_dim, t->grad_x_stride_token, t->grad_x_stride_head)) return LIBRA_INVALID_ARGUMENT;
-    if (t->grad_x == t->x && (t->x_stride_token != t->grad_x_stride_token || t->x_stride_head != t->grad_x_stride_head)) return LIBRA_INVALID_ARGUMENT;
-    if (t->grad_x == t->grad_out &&
+    if (t->x && t->grad_x == t->x && (t->x_stride_token != t->grad_x_stride_token || t->x_stride_head != t->grad_x_stride_head)) return LIBRA_INVALID_ARGUMENT;
+    if (t->grad_x && t->grad_x == t->grad_out &&
         (t->grad_out_stride_token != t->grad_x_stride_token || t->grad_out_stride_head != t->grad_x_stride_head)) {
       return LIBRA_INVALID_ARGUMENT;
     }
