@@ -684,6 +684,7 @@ int libra_norm_rope_gradient(int32_t device, const libra_rope_t* rope, const lib
  *   slots         int32[max_rows]: page * page_size + place in the page; -1: the row's k and v are not stored
  *   n_rows        device word with the number of rows, e.g. &q_offsets[batch], or NULL: max_rows of them.  Rows behind it are
  *                 left as they were
+ * For max_rows 0 the arrays of rows may be NULL, as the addresses of empty arrays are.
  * No two rows of a call may name the same slot.  A slot outside the pool sets LIBRA_ERR_BAD_PAGE_ID and is not stored.  E4M3 pools
  * as in libra_rope_append.  The handle supplies the pool geometry and type; no plan, no workspace.  Asynchronous on `stream`; may be
  * recorded.  Errors: as libra_rope_append; UNSUPPORTED_SHAPE also for num_pages * page_size > 2^31 - 1. */

@@ -270,8 +270,9 @@ int libra_norm_rope_append(libra_handle_t h, const libra_rope_t* rope, const voi
                            const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new,
                            int64_t kv_stride, const int32_t* positions, const int32_t* slots, const int32_t* n_rows, int32_t max_rows,
                            void* k_pages, void* v_pages, void* error_word_dev, void* stream) {
-  if (!h || !k_new || !v_new || !slots || !k_pages || !v_pages || !error_word_dev || max_rows < 0) return LIBRA_INVALID_ARGUMENT;
-  if ((q == nullptr) != (q_out == nullptr) || (rope && (!valid_rope(rope) || !positions))) return LIBRA_INVALID_ARGUMENT;
+  if (!h || !k_pages || !v_pages || !error_word_dev || max_rows < 0) return LIBRA_INVALID_ARGUMENT;
+  if (max_rows > 0 && (!k_new || !v_new || !slots || (rope && !positions))) return LIBRA_INVALID_ARGUMENT;   // no row is read where there is none
+  if ((max_rows > 0 && (q == nullptr) != (q_out == nullptr)) || (rope && !valid_rope(rope))) return LIBRA_INVALID_ARGUMENT;
   if (!std::isnormal(eps) || eps < 0.f) return LIBRA_INVALID_ARGUMENT;
   const int D = h->cfg.head_dim;
   const int64_t q_row = int64_t(h->cfg.num_q_heads) * D, kv_row = int64_t(h->cfg.num_kv_heads) * D;

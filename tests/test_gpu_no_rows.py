@@ -28,3 +28,16 @@ def test_norms(lib, dim, rotary):
     ws = torch.empty(lib.libra_norm_rope_workspace_size(0, dim), dtype=torch.uint8, device="cuda")
     lib.libra_norm_rope_gradient(0, rope, q, k, lib.ROPE_F32, pos.data_ptr(), 0, dim, EPS, ws.data_ptr(), ws.numel(), stream())
     assert all(bool((g == 0).all()) for g in gw)
+
+
+def test_append(lib):
+    import torch
+    h = lib.Handle(4, 2, 64, 3, 1, 4)
+    kv = torch.full((3, 2, 16, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    x, i, err = torch.empty((0, 8, 64), dtype=torch.bfloat16, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    w, out = torch.ones(64, dtype=torch.bfloat16, device="cuda"), torch.empty((0, 4, 64), dtype=torch.bfloat16, device="cuda")
+    for rope in (None, rope_of(lib, 64)):
+        h.norm_rope_append(rope, w.data_ptr(), w.data_ptr(), EPS, x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), x.data_ptr(), x.data_ptr(),
+                           x.stride(0), i.data_ptr(), i.data_ptr(), 0, 0, kv.data_ptr(), kv.data_ptr(), err.data_ptr(), stream())
+    assert int(err) == 0 and bool((kv == 7).all())
+    h.close()
