@@ -599,9 +599,10 @@ int libra_chunk_attn(libra_handle_t handle, const void* q, int64_t q_stride, con
  * pages are a stack in device memory, free_pages[0 .. *free_count), int32[num_pages], filled by the caller once with the
  * pages that no sequence owns.  Pages have one owner each.  Both calls need no plan and no workspace, take at most 4096 sequences
  * and launch one kernel; integers, the same result every time.  All pointers are device pointers; seq_lens, block_table, free_pages
- * and free_count change in place and must not overlap one another or an input.  If a check on the device fails, error bits are set
- * in *error_word_dev (32-bit device word) and NOTHING is changed, except that libra_cache_extend's q_offsets become all zero, so
- * that the calls that go by them find no new rows (the attention goes by its plan):
+ * and free_count change in place and must not overlap one another or an input.  For batch 0 new_tokens (keep_lens), seq_lens and
+ * block_table may be NULL, as the addresses of empty arrays are.  If a check on the device fails, error bits are set in *error_word_dev
+ * (32-bit device word) and NOTHING is changed, except that libra_cache_extend's q_offsets become all zero, so that the calls that go
+ * by them find no new rows (the attention goes by its plan):
  *   LIBRA_ERR_BAD_LENGTH     a negative length or number of tokens, more kept than there are, *free_count outside [0, num_pages],
  *                            more pages going back than the pool has room for
  *   LIBRA_ERR_PLAN_OVERFLOW  a length past the end of a block-table row (or past 2^31 - 1), more than max_rows new rows

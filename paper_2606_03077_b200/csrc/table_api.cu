@@ -19,12 +19,13 @@ bool off(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a !=
 // What both calls check, and the parameters they share.
 int common(libra_handle_t h, const int32_t* change, int32_t* seq_lens, int32_t* block_table, int32_t batch, int32_t* free_pages,
            int32_t* free_count, void* error_word_dev, libra::TableParams* p) {
-  if (!h || !change || !seq_lens || !block_table || !free_pages || !free_count || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
+  if (!h || !free_pages || !free_count || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
   if (batch < 0 || batch > h->cfg.max_batch) return LIBRA_INVALID_ARGUMENT;
+  if (batch > 0 && (!change || !seq_lens || !block_table)) return LIBRA_INVALID_ARGUMENT;   // not read where there are no sequences
   if (off(change, 4) || off(seq_lens, 4) || off(block_table, 4) || off(free_pages, 4) || off(free_count, 4) || off(error_word_dev, 4)) {
     return LIBRA_INVALID_ARGUMENT;
   }
-  if (change == seq_lens) return LIBRA_INVALID_ARGUMENT;   // other blocks may still be reading the one while the other is written
+  if (batch > 0 && change == seq_lens) return LIBRA_INVALID_ARGUMENT;   // other blocks may still be reading the one while the other is written
   if (batch > libra::kTableMaxBatch) return LIBRA_UNSUPPORTED_SHAPE;
   if (h->cfg.num_pages > 0x7fffffff / h->cfg.page_size) return LIBRA_UNSUPPORTED_SHAPE;   // a slot's number
   *p = {};

@@ -41,3 +41,15 @@ def test_append(lib):
                            x.stride(0), i.data_ptr(), i.data_ptr(), 0, 0, kv.data_ptr(), kv.data_ptr(), err.data_ptr(), stream())
     assert int(err) == 0 and bool((kv == 7).all())
     h.close()
+
+
+def test_tables(lib):
+    import torch
+    h = lib.Handle(4, 2, 64, 3, 1, 4)
+    none, one = torch.empty(0, dtype=torch.int32, device="cuda").data_ptr(), torch.zeros(4, dtype=torch.int32, device="cuda")
+    free, count, off = torch.arange(3, dtype=torch.int32, device="cuda"), torch.tensor([3], dtype=torch.int32, device="cuda"), torch.full((2,), -7, dtype=torch.int32, device="cuda")
+    h.cache_extend(none, none, none, 0, free.data_ptr(), count.data_ptr(), off.data_ptr(), none, none, 0, one.data_ptr(), stream())
+    assert off.tolist() == [0, -7] and int(count) == 3
+    h.cache_trim(none, none, none, 0, free.data_ptr(), count.data_ptr(), one.data_ptr(), stream())
+    assert int(count) == 3 and one.tolist() == [0] * 4 and free.tolist() == [0, 1, 2]
+    h.close()
