@@ -699,7 +699,8 @@ int libra_norm_rope_append(libra_handle_t handle, const libra_rope_t* rope, cons
  * before its children, and attends with every token to the cached ones, to its ancestors and to itself:
  *   libra_cache_extend -> libra_tree_mask -> (each layer: libra_norm_rope_append, libra_tree_attn) -> the caller accepts a path
  *   -> (each layer: libra_tree_keep) -> libra_cache_trim
- * The new tokens are packed as above (q_offsets; seq_lens counts them).
+ * The new tokens are packed as above (q_offsets; seq_lens counts them).  Where there are no new tokens (max_rows 0, a plan without any) or
+ * no sequences, the arrays that go by them may be NULL, as the addresses of empty arrays are.
  *
  * libra_tree_mask: parents[r], for row r = q_offsets[b] + i, is the place (0 .. i - 1) of the token's parent among its sequence's new
  * ones, or -1: it follows the last cached token.  Bit j % 32 of word mask[r * mask_ld + j / 32] is set where j = i or j is an

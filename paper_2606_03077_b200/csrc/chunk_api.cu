@@ -63,10 +63,14 @@ int set_attributes(libra_handle_t h) {
   return LIBRA_OK;
 }
 
+// The plan has no new tokens: what goes by rows or sequences is not read, and may be an empty array's null.
+bool nothing_planned(libra_handle_t h) { return h && h->chunk.planned && h->chunk.n_items == 0; }
+
 // Both attentions; mask null: a chain.
 int attend(libra_handle_t h, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages, const int32_t* block_table,
            const uint32_t* mask, int32_t mask_ld, void* out, float* lse, void* error_word_dev, void* stream) {
-  if (!h || !q || !k_pages || !v_pages || !block_table || !out || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
+  if (!h || !k_pages || !v_pages || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
+  if (!nothing_planned(h) && (!q || !block_table || !out)) return LIBRA_INVALID_ARGUMENT;
   if (q_stride < int64_t(h->cfg.num_q_heads) * h->cfg.head_dim || q_stride % 8 != 0) return LIBRA_INVALID_ARGUMENT;
   auto off = [](const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; };
   if (off(q, 16) || off(k_pages, 16) || off(v_pages, 16) || off(out, 16) || off(block_table, 4) || off(lse, 4) || off(error_word_dev, 4)) {
@@ -274,7 +278,7 @@ int libra_chunk_attn(libra_handle_t h, const void* q, int64_t q_stride, const vo
 int libra_tree_attn(libra_handle_t h, const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
                     const int32_t* block_table, const uint32_t* mask, int32_t mask_ld, void* out, float* lse, void* error_word_dev,
                     void* stream) {
-  if (!mask || mask_ld <= 0 || reinterpret_cast<uintptr_t>(mask) % 4 != 0) return LIBRA_INVALID_ARGUMENT;
+  if ((!mask && !nothing_planned(h)) || mask_ld <= 0 || reinterpret_cast<uintptr_t>(mask) % 4 != 0) return LIBRA_INVALID_ARGUMENT;
   return attend(h, q, q_stride, k_pages, v_pages, block_table, mask, mask_ld, out, lse, error_word_dev, stream);
 }
 

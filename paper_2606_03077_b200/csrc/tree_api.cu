@@ -21,8 +21,9 @@ extern "C" {
 
 int libra_tree_mask(libra_handle_t h, const int32_t* parents, const int32_t* q_offsets, const int32_t* seq_lens, int32_t batch,
                     int32_t max_rows, uint32_t* mask, int32_t mask_ld, int32_t* positions, void* error_word_dev, void* stream) {
-  if (!h || !parents || !q_offsets || !seq_lens || !mask || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
+  if (!h || !q_offsets || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
   if (batch < 0 || batch > h->cfg.max_batch || max_rows < 0 || mask_ld <= 0) return LIBRA_INVALID_ARGUMENT;
+  if ((batch > 0 && !seq_lens) || (max_rows > 0 && (!parents || !mask))) return LIBRA_INVALID_ARGUMENT;
   if (off(parents, 4) || off(q_offsets, 4) || off(seq_lens, 4) || off(mask, 4) || off(positions, 4) || off(error_word_dev, 4)) {
     return LIBRA_INVALID_ARGUMENT;
   }
@@ -48,15 +49,14 @@ int libra_tree_mask(libra_handle_t h, const int32_t* parents, const int32_t* q_o
 int libra_tree_keep(libra_handle_t h, const int32_t* kept, int32_t kept_ld, const int32_t* n_kept, const int32_t* q_offsets,
                     const int32_t* seq_lens, const int32_t* block_table, int32_t batch, void* k_pages, void* v_pages,
                     int32_t* new_lens, void* error_word_dev, void* stream) {
-  if (!h || !kept || !n_kept || !q_offsets || !seq_lens || !block_table || !k_pages || !v_pages || !error_word_dev) {
-    return LIBRA_INVALID_ARGUMENT;
-  }
+  if (!h || !q_offsets || !k_pages || !v_pages || !error_word_dev) return LIBRA_INVALID_ARGUMENT;
   if (batch < 0 || batch > h->cfg.max_batch || kept_ld <= 0) return LIBRA_INVALID_ARGUMENT;
+  if (batch > 0 && (!kept || !n_kept || !seq_lens || !block_table)) return LIBRA_INVALID_ARGUMENT;
   if (off(kept, 4) || off(n_kept, 4) || off(q_offsets, 4) || off(seq_lens, 4) || off(block_table, 4) || off(k_pages, 16) ||
       off(v_pages, 16) || off(new_lens, 4) || off(error_word_dev, 4)) {
     return LIBRA_INVALID_ARGUMENT;
   }
-  if (new_lens == seq_lens) return LIBRA_INVALID_ARGUMENT;   // other blocks of the sequence may not have read its length yet
+  if (batch > 0 && new_lens == seq_lens) return LIBRA_INVALID_ARGUMENT;   // other blocks of the sequence may not have read its length yet
   if (batch == 0) return LIBRA_OK;
   DeviceGuard guard(h->cfg.device);
   if (guard.err != cudaSuccess) return fail_cuda(h, guard.err);

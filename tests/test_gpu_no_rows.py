@@ -53,3 +53,24 @@ def test_tables(lib):
     h.cache_trim(none, none, none, 0, free.data_ptr(), count.data_ptr(), one.data_ptr(), stream())
     assert int(count) == 3 and one.tolist() == [0] * 4 and free.tolist() == [0, 1, 2]
     h.close()
+
+
+def test_trees(lib):
+    import torch
+    h = lib.Handle(4, 2, 64, 3, 2, 4)
+    z = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    kv, err, none = torch.full((3, 2, 16, 64), 7.0, dtype=torch.bfloat16, device="cuda"), z(1), torch.empty(0, dtype=torch.int32, device="cuda").data_ptr()
+    p, s = kv.data_ptr(), stream()
+    # sequences without new tokens
+    off, lens, bt = z(3), torch.tensor([5, 9], dtype=torch.int32, device="cuda"), z(2, 4)
+    h.tree_mask(none, off.data_ptr(), lens.data_ptr(), 2, 0, none, 1, none, err.data_ptr(), s)
+    ws = torch.empty(h.chunk_workspace_size(1), dtype=torch.uint8, device="cuda")
+    h.chunk_plan([0, 0], [5, 9], ws.data_ptr(), ws.numel(), s)
+    h.tree_attn(none, 256, p, p, bt.data_ptr(), none, 1, none, none, err.data_ptr(), s)
+    # no sequences
+    h.tree_mask(none, z(1).data_ptr(), none, 0, 0, none, 1, none, err.data_ptr(), s)
+    h.tree_keep(none, 1, none, z(1).data_ptr(), none, none, 0, p, p, none, err.data_ptr(), s)
+    h.chunk_plan([], [], ws.data_ptr(), ws.numel(), s)
+    h.tree_attn(none, 256, p, p, none, none, 1, none, none, err.data_ptr(), s)
+    assert int(err) == 0 and bool((kv == 7).all())
+    h.close()
