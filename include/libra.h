@@ -658,7 +658,8 @@ int libra_norm_rope_apply(int32_t device, const libra_rope_t* rope, const libra_
                           int32_t dtype, const int32_t* positions, int64_t n_tokens, int32_t head_dim, float eps, void* stream);
 
 /* The gradient of libra_norm_rope_apply from its inputs (x, weight) and the gradient of its output.  grad_x [n_tokens, n_heads,
- * head_dim] of `dtype` may be grad_out or x (with the same strides); grad_weight: float32[head_dim], overwritten (zero for no tokens).
+ * head_dim] of `dtype` may be grad_out or x (with the same strides); grad_weight: float32[head_dim], overwritten (zero for no tokens); k's
+ * is an array of its own, also where q and k share their weight (its gradient is then the sum of both).
  * workspace_dev: libra_norm_rope_workspace_size bytes on the device, 16-byte aligned, for the sums of the blocks; calls that can
  * overlap need one each, replays of recorded calls too.  grad_weight is summed in a fixed order: the same bits every time.
  * Errors: as above, WORKSPACE_TOO_SMALL. */

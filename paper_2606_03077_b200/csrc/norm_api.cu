@@ -153,6 +153,7 @@ int libra_norm_rope_apply(int32_t device, const libra_rope_t* rope, const libra_
            aligned(t->weight, 16);
   }
   if (n_tokens == 0) return LIBRA_OK;
+  if (k && k->out == q->out) return LIBRA_INVALID_ARGUMENT;
   DeviceGuard guard(device);
   if (guard.err != cudaSuccess) return fail_cuda(nullptr, guard.err);
   int n_sm = 0;
@@ -227,6 +228,7 @@ int libra_norm_rope_gradient(int32_t device, const libra_rope_t* rope, const lib
            wide_rows(t->grad_out, t->grad_out_stride_token, t->grad_out_stride_head, v) &&
            wide_rows(t->grad_x, t->grad_x_stride_token, t->grad_x_stride_head, v) && aligned(t->weight, 16);
   }
+  if (k && (k->grad_weight == q->grad_weight || (n_tokens > 0 && k->grad_x == q->grad_x))) return LIBRA_INVALID_ARGUMENT;   // neither adds to the other
   DeviceGuard guard(device);
   if (guard.err != cudaSuccess) return fail_cuda(nullptr, guard.err);
   int n_sm = 0;
