@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_extend_kernel(const Ta
       }
     }
   }
+  __syncwarp();   // the lanes' loops differ in length, and the barrier is one instruction of whole warps
   if (ranks > 1) cluster_wait();
   if (rank == 0) {
 #pragma unroll
@@ -295,6 +296,7 @@ __global__ void __launch_bounds__(kTableMaxThreads) cache_trim_kernel(const Tabl
     const int b = owner_of(page_begin, p.batch, int32_t(k));
     p.free_pages[count + total.pages - 1 - k] = p.block_table[int64_t(b) * p.block_table_ld + left[b] + (k - page_begin[b])];
   }
+  __syncwarp();   // the lanes' loops differ in length, and the barrier is one instruction of whole warps
   if (ranks > 1) cluster_wait();
   if (rank == 0) {
 #pragma unroll
