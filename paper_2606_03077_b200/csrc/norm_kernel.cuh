@@ -9,7 +9,7 @@
 //
 // Every byte moves once; memory bounds it.  A step is the rows (heads) of one token and one kind (q, k, v) that a warp holds at once: a
 // row is held by a group of neighbouring lanes, each with one item of two vectors (of 16 bytes, or 8) whose channels turn together (half layout:
-// R / 2 apart), so that a row's sums take one reduction within the group and nothing but cosines goes from lane to lane.  Every warp
+// R / 2 apart), so that a row's sum takes one reduction within the group (the gradient's two) and nothing but cosines goes from lane to lane.  Every warp
 // takes a run of consecutive steps, without a barrier of the block: a token's cosines and sines are worked out once in the run, by all
 // lanes, and multiplied by the weights into four factors a pair, so that norm, weight and rotation are six multiplications a pair, two
 // pairs an instruction.  Rows that this does not fit (rotated parts or heads that the items do not divide, addresses off a 16-byte boundary, heads of
@@ -20,10 +20,12 @@
 //
 // dw is summed in registers along a warp's run, then over the warps and the blocks in a fixed order: the same bits every time.
 //
-// Measured (device, changing inputs): 8191 tokens of 40 + 8 heads of 128, fp16, half of each rotated, 36 us = 5.6 TB/s; gradient of 16384
-// tokens of 32 + 8 heads, bf16, 83 us = 6.1 TB/s, of which 2 - 3 are the sums of the blocks (a kernel of its own); 16K tokens of 64 + 8 heads
-// into an E4M3 cache 109 us = 5.8 TB/s.  A step is 215 instructions forward and 310 backward; with few heads a token's own share of
-// them (factors, addresses) shows: 8192 tokens of 16 + 4 heads 20 us, 4.2 TB/s.  q and k of 64 tokens: 2.8 us.
+// Measured (device, changing inputs): 8191 tokens of 40 + 8 heads of 128, fp16, half of each rotated, 36 us = 5.6 TB/s; 16384 of the same
+// in bf16, all channels rotated in halves, 68 - 74 us = 5.4 - 5.9 TB/s; 8192 tokens of 32 + 8 heads in float32 63 us = 5.3 TB/s; gradient of
+// 16384 tokens of 32 + 8 heads, bf16, 85.5 us = 5.9 TB/s, of which 2 - 3 are the sums of the blocks (a kernel of its own; with both sums
+// of a row in one reduction, of w g x, which leaves float32's range where the result does not: 82.4); the same bytes in float32 91 us; 16K
+// tokens of 64 + 8 heads into an E4M3 cache 109 us = 5.8 TB/s.  A step is 215 instructions forward and 317 backward; with few heads a
+// token's own share of them (factors, addresses) shows: 8192 tokens of 16 + 4 heads 20 us, 4.2 TB/s.  q and k of 64 tokens: 3 us.
 // What did not do as well, on the three above (us): rows straight into registers, two a lane 41 / 128 / 157 (spills), four 43 / 158 / 143;
 // every 32nd row a warp's, with the factors in shared memory 55 / 134 / 208; interleaved items of two neighbouring vectors 53 for the
 // first (each sector asked for twice); gradient blocks for q or k alone 106.
